@@ -14,6 +14,8 @@
  *                                              distinct ids (nanospec_set_stream_policy)
  *   Sec 4.2 softmax over the active set only   log-probabilities with the selection
  *                                              (nanospec_topk_logprob_remap)
+ * and, beside the paper: heads on weights kept in 8 bits, and log-probabilities of given tokens with the losses that
+ * train a draft (or a policy) on the logits of a head.
  *
  * Conventions
  *   - Token ids are 0-based int32 in [0, V).
@@ -292,6 +294,98 @@ NANOSPEC_API nanospec_status nanospec_dense_topk(const float* d_logits, int32_t 
 NANOSPEC_API int64_t nanospec_dense_topk_static_limit(void);
 NANOSPEC_API nanospec_status nanospec_dense_topk_static(const float* d_logits, int32_t V, int32_t M_total, int32_t k,
                                                         int32_t* d_out_ids, float* d_out_vals, void* hip_stream);
+
+/* Heads on 8-bit weights: the bytes of W_head bound the heads above, 8 bits halve them.  Every row is kept as int8 with a
+ * scale of its own,
+ *   a = max_c |x_c|, scale = a / 127, q_c = 127 x_c / a rounded to the nearest integer, ties to even (|q| <= 127),
+ * the quotient rounded once: q is what exact arithmetic on the bf16 values gives.  A row of zeros has q = 0 and scale 0, a row that
+ * holds an infinity or a NaN q = 0 and scale NaN (all logits it meets are NaN).
+ *   nanospec_quantize_rows : d_Q int8 [rows][d] and d_scale fp32 [rows] from d_X bf16 [rows][d]; of the weights, once.
+ *   nanospec_dense_head_i8 : logits[m][v] = scale_H[m] scale_W[v] sum_c qH[m][c] qW[v][c] for all v < V, where qH, scale_H are the
+ *                            hidden rows d_H_bf16 [M_total][d] quantized by the call in the same way (a scale per token) and
+ *                            qW, scale_W the weights' (a scale per vocabulary row).  The sum is taken in 32-bit integers and is
+ *                            exact; it is rounded to fp32 and multiplied with the two scales: logits do not depend on the kernel that
+ *                            ran.  Layout as nanospec_dense_head.
+ *   nanospec_sparse_head_i8: the same on the active rows, layout as nanospec_sparse_head: d_H_bf16 [batch][M][d] -> d_logits fp32
+ *                            [batch][M][capacity]; entries j >= n_b are left as they were.  V and d are the state's.
+ *   d_workspace : device scratch of at least nanospec_head_i8_workspace(rows, d) bytes, rows = M_total or batch * M (-1: sizes out
+ *                 of range), 256-byte aligned; asked for whatever the sizes.  Calls that may overlap (two streams, two captured
+ *                 graphs) must not share one.
+ * Limits: d a multiple of 16 and at most 133136 (the sum fits 32 bits); V * d and rows * d below 2^32; d_W_i8, d_Q, d_H_bf16
+ * and d_X_bf16 16-byte aligned.
+ * Errors: EINVAL (null, sizes < 1, a limit exceeded), ECAPACITY (M > m_cap, workspace too small), EHIP.  Asynchronous. */
+NANOSPEC_API nanospec_status nanospec_quantize_rows(const void* d_X_bf16, int64_t rows, int32_t d, int8_t* d_Q, float* d_scale,
+                                                    void* hip_stream);
+NANOSPEC_API int64_t nanospec_head_i8_workspace(int32_t rows, int32_t d);
+NANOSPEC_API nanospec_status nanospec_dense_head_i8(const int8_t* d_W_i8, const float* d_W_scale, const void* d_H_bf16, int32_t V,
+                                                    int32_t d, int32_t M_total, float* d_logits, void* d_workspace,
+                                                    int64_t workspace_bytes, void* hip_stream);
+NANOSPEC_API nanospec_status nanospec_sparse_head_i8(nanospec_state* st, const int8_t* d_W_i8, const float* d_W_scale,
+                                                     const void* d_H_bf16, int32_t M, float* d_logits, void* d_workspace,
+                                                     int64_t workspace_bytes, void* hip_stream);
+
+/* Rows of logits with a token each: what the calls below work on.  The struct is read before they return.
+ *   d_logits      : [rows][ld] of `type`, columns 0 .. V-1 (those of nanospec_dense_head with ld = V; of nanospec_sparse_head with
+ *                   ld = V = capacity, rows = batch * M).
+ *   d_tokens      : int32 [rows], global ids.
+ *   d_ids, d_n    : NULL: column j is id j.  Else the active sets, as nanospec_vocab_view gives them: row r's columns are the
+ *                   ids d_ids[(r / rows_per_list) * V + j] for j < d_n[r / rows_per_list], ascending (rows_per_list = M); the
+ *                   distribution is renormalised over them, as in nanospec_topk_logprob_remap.  Columns behind are neither read nor
+ *                   written.
+ * A logit of -inf has probability 0.  A token has no probability if it has no column, if its logit is -inf, or if exp of its
+ * log-probability is 0 in 64 bits (below -745); a NaN or +inf among the columns of a row makes the row's results NaN. */
+#define NANOSPEC_F32 0
+#define NANOSPEC_BF16 1
+typedef struct nanospec_logit_rows {
+  const void* d_logits;
+  const int32_t* d_tokens;
+  const int32_t* d_ids;
+  const int32_t* d_n;
+  int64_t ld;            /* row stride in elements, >= V */
+  int32_t type;          /* NANOSPEC_F32 or NANOSPEC_BF16 */
+  int32_t rows;
+  int32_t V;             /* columns; row stride of d_ids */
+  int32_t rows_per_list; /* hidden rows per active set; ignored without d_ids */
+} nanospec_logit_rows;
+
+/* Log-probabilities of given tokens (a verifier's or a reference model's view of an answer; the draft's own probabilities of what
+ * it proposed, which rejection sampling needs):
+ *   logprob[r] = z_r[token] - log sum_j exp(z_r[j]), -inf where the token has no column or its logit is -inf.
+ * Losses on the logits of a head, each with the gradient of those logits.  With w_r = d_weight[r] (fp32 [rows]; NULL: 1), a
+ * row counts if w_r is not 0; rows that do not count are not read, whatever they hold.  log p_r as above, in fp32 -- max and sums -- and
+ * 64 bits behind the sums; every sum has a fixed order, so that results are reproducible bit for bit.
+ *   nanospec_policy_loss: the clipped policy loss with a KL term,
+ *     ratio = exp(log p_r - d_old[r]), gap = d_ref[r] - log p_r, A = d_adv[r],
+ *     row_loss[r] = -min(ratio A, clamp(ratio, 1 - clip_low, 1 + clip_high) A) + kl_beta (exp(gap) - gap - 1),
+ *     loss = sum of w_r row_loss[r] over the rows that count (a mean over tokens or answers is a matter of the weights).
+ *     d_ref may be NULL if kl_beta is 0.  A row whose token has no probability has row_loss 0 and no gradient.
+ *   nanospec_preference_loss: the preference loss on `pairs` pairs of answers.  Answer q covers rows h_off[q] .. h_off[q+1), pair p
+ *     is answer 2p, the chosen one, and 2p + 1, the rejected one; rows outside h_off[0] .. h_off[2 pairs) do not count;
+ *     S_q = sum of w_r (log p_r - d_ref[r]) (d_ref NULL: 0; a row whose token has no probability adds nothing),
+ *     margin[p] = beta (S_2p - S_2p+1), loss = mean over p of -(1 - smoothing) log sigma(margin) - smoothing log sigma(-margin).
+ *     h_off: host int32 [2 pairs + 1], non-decreasing, within 0 .. rows, read before the call returns; 2 pairs <= NANOSPEC_MAX_BATCH.
+ *   d_loss fp32 [1]; d_row_loss [rows], d_margin [pairs], d_logprob [rows]: fp32, each may be NULL.  row_loss and logprob of rows that
+ *     do not count are 0.
+ *   d_grad : NULL: none.  Else [rows][ld_grad] of grad_type: grad_scale * dloss/dz for every row and its live columns, zeros in rows
+ *     that do not count.  It may be the logits' own memory if type and stride are the same, and must not overlap them else.
+ *   d_workspace : device scratch of at least nanospec_loss_workspace(rows, V) bytes (-1: sizes out of range), 256-byte aligned.  Calls
+ *     that may overlap must not share one.
+ * Limits: rows * ld below 2^60, V <= 2^30.  Errors: EINVAL (null, sizes < 1, ld < V, an unknown type, d_ids without d_n or
+ * the other way round, clip_low or clip_high negative, kl_beta != 0 without d_ref, smoothing outside [0, 1], a NaN among these, bad
+ * offsets), ECAPACITY (workspace too small, 2 pairs > NANOSPEC_MAX_BATCH), EHIP.  Asynchronous. */
+NANOSPEC_API int64_t nanospec_loss_workspace(int32_t rows, int32_t V);
+NANOSPEC_API nanospec_status nanospec_token_logprob(const nanospec_logit_rows* rows, float* d_logprob, void* d_workspace,
+                                                    int64_t workspace_bytes, void* hip_stream);
+NANOSPEC_API nanospec_status nanospec_policy_loss(const nanospec_logit_rows* rows, const float* d_old, const float* d_ref,
+                                                  const float* d_adv, const float* d_weight, float clip_low, float clip_high,
+                                                  float kl_beta, float* d_loss, float* d_row_loss, float* d_logprob, void* d_grad,
+                                                  int32_t grad_type, int64_t ld_grad, float grad_scale, void* d_workspace,
+                                                  int64_t workspace_bytes, void* hip_stream);
+NANOSPEC_API nanospec_status nanospec_preference_loss(const nanospec_logit_rows* rows, const int32_t* h_off, int32_t pairs,
+                                                      const float* d_ref, const float* d_weight, float beta, float smoothing,
+                                                      float* d_loss, float* d_margin, float* d_logprob, void* d_grad,
+                                                      int32_t grad_type, int64_t ld_grad, float grad_scale, void* d_workspace,
+                                                      int64_t workspace_bytes, void* hip_stream);
 
 /* Measurement aids, not part of the method: read-only kernels that move the bytes the head moves and
  * compute nothing, to measure what one launch of that size and access pattern can reach on the chip.

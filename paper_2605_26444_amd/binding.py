@@ -28,13 +28,23 @@ EXPORTS = [
     "nanospec_packed_bytes", "nanospec_packed_enable", "nanospec_packed_gather", "nanospec_packed_head", "nanospec_packed_view",
     "nanospec_union_bytes", "nanospec_union_enable", "nanospec_union_build", "nanospec_union_head", "nanospec_union_view",
     "nanospec_calib_stream_read", "nanospec_calib_gather_read", "nanospec_calib_valu_head", "nanospec_last_device_error",
+    "nanospec_quantize_rows", "nanospec_head_i8_workspace", "nanospec_dense_head_i8", "nanospec_sparse_head_i8",
+    "nanospec_loss_workspace", "nanospec_token_logprob", "nanospec_policy_loss", "nanospec_preference_loss",
 ]
+F32, BF16 = 0, 1
 
 
 class Layout(C.Structure):
     _fields_ = [(n, C.c_int64) for n in (
         "ring_bytes", "counter_bytes", "window_bitmap_bytes", "topk_bitmap_bytes", "ids_bytes", "scalars_bytes",
         "workspace_bytes", "total_bytes", "gathered_bytes_at_cap")] + [("capacity", C.c_int32)]
+
+
+class LogitRows(C.Structure):
+    """nanospec_logit_rows; `keep` holds the tensors whose addresses it carries"""
+    _fields_ = [("d_logits", C.c_void_p), ("d_tokens", C.c_void_p), ("d_ids", C.c_void_p), ("d_n", C.c_void_p), ("ld", C.c_int64),
+                ("type", C.c_int32), ("rows", C.c_int32), ("V", C.c_int32), ("rows_per_list", C.c_int32)]
+    keep = None
 
 
 class NanoSpecError(RuntimeError):
@@ -92,9 +102,20 @@ def lib() -> C.CDLL:
         L.nanospec_union_head.argtypes = [vp, vp, vp, i32, vp, vp]
         L.nanospec_union_view.argtypes = [vp] + [C.POINTER(vp)] * 6 + [i32p, i32p]
         L.nanospec_last_device_error.argtypes = [vp, i32p, vp]
+        f32 = C.c_float
+        L.nanospec_quantize_rows.argtypes = [vp, i64, i32, vp, vp, vp]
+        L.nanospec_head_i8_workspace.restype = i64
+        L.nanospec_head_i8_workspace.argtypes = [i32, i32]
+        L.nanospec_dense_head_i8.argtypes = [vp, vp, vp, i32, i32, i32, vp, vp, i64, vp]
+        L.nanospec_sparse_head_i8.argtypes = [vp, vp, vp, vp, i32, vp, vp, i64, vp]
+        L.nanospec_loss_workspace.restype = i64
+        L.nanospec_loss_workspace.argtypes = [i32, i32]
+        L.nanospec_token_logprob.argtypes = [C.POINTER(LogitRows), vp, vp, i64, vp]
+        L.nanospec_policy_loss.argtypes = [C.POINTER(LogitRows), vp, vp, vp, vp, f32, f32, f32, vp, vp, vp, vp, i32, i64, f32, vp, i64, vp]
+        L.nanospec_preference_loss.argtypes = [C.POINTER(LogitRows), vp, i32, vp, vp, f32, f32, vp, vp, vp, vp, i32, i64, f32, vp, i64, vp]
         for name in EXPORTS:
             if name not in ("nanospec_status_string", "nanospec_dense_topk_workspace", "nanospec_dense_topk_static_limit",
-                            "nanospec_packed_bytes", "nanospec_union_bytes"):
+                            "nanospec_packed_bytes", "nanospec_union_bytes", "nanospec_head_i8_workspace", "nanospec_loss_workspace"):
                 getattr(L, name).restype = i32
         _lib = L
     return _lib
@@ -288,6 +309,83 @@ def nanospec_union_view(st):
     cap, share = C.c_int32(), C.c_int32()
     _check(lib().nanospec_union_view(st, *[C.byref(x) for x in ptrs], C.byref(cap), C.byref(share)), "nanospec_union_view")
     return tuple(x.value for x in ptrs) + (cap.value, share.value)
+
+
+def nanospec_quantize_rows(d_X, rows, d, d_Q, d_scale, stream=None):
+    _check(lib().nanospec_quantize_rows(_ptr(d_X), rows, d, _ptr(d_Q), _ptr(d_scale), _stream(stream)), "nanospec_quantize_rows")
+
+
+def nanospec_head_i8_workspace(rows, d) -> int:
+    return int(lib().nanospec_head_i8_workspace(rows, d))
+
+
+def nanospec_dense_head_i8(d_W, d_W_scale, d_H, V, d, M_total, d_logits, d_workspace, workspace_bytes, stream=None):
+    _check(lib().nanospec_dense_head_i8(_ptr(d_W), _ptr(d_W_scale), _ptr(d_H), V, d, M_total, _ptr(d_logits), _ptr(d_workspace), workspace_bytes,
+                                        _stream(stream)), "nanospec_dense_head_i8")
+
+
+def nanospec_sparse_head_i8(st, d_W, d_W_scale, d_H, M, d_logits, d_workspace, workspace_bytes, stream=None):
+    _check(lib().nanospec_sparse_head_i8(st, _ptr(d_W), _ptr(d_W_scale), _ptr(d_H), M, _ptr(d_logits), _ptr(d_workspace), workspace_bytes,
+                                         _stream(stream)), "nanospec_sparse_head_i8")
+
+
+def _type_and_stride(t):
+    """(type code, row stride) of a [rows][columns] tensor whose columns lie side by side"""
+    name = str(t.dtype)
+    if name not in ("torch.float32", "torch.bfloat16"):
+        raise ValueError(f"logits and their gradients are float32 or bfloat16, not {name}")
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or not t.is_cuda:
+        raise ValueError("logits and their gradients are device tensors [rows][columns] with columns side by side")
+    return (F32 if name == "torch.float32" else BF16), (t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1]))
+
+
+def logit_rows(d_logits, d_tokens, V=None, ids=None, n=None, rows_per_list=1) -> LogitRows:
+    """nanospec_logit_rows of a [rows][columns] tensor (rows may be strided) and its tokens.  ids, n: the active sets, as
+    nanospec_vocab_view gives them; V: columns, all of the tensor's if not given."""
+    kind, ld = _type_and_stride(d_logits)
+    if d_tokens.numel() < d_logits.shape[0] or str(d_tokens.dtype) != "torch.int32":
+        raise ValueError("a token (int32) for every row of logits is needed")
+    r = LogitRows(d_logits.data_ptr(), _ptr(d_tokens), _ptr(ids), _ptr(n), ld, kind, d_logits.shape[0], d_logits.shape[1] if V is None else V, rows_per_list)
+    r.keep = (d_logits, d_tokens, ids, n)
+    return r
+
+
+def nanospec_loss_workspace(rows, V) -> int:
+    return int(lib().nanospec_loss_workspace(rows, V))
+
+
+def nanospec_token_logprob(rows, d_logprob, d_workspace, workspace_bytes, stream=None):
+    _check(lib().nanospec_token_logprob(rows, _ptr(d_logprob), _ptr(d_workspace), workspace_bytes, _stream(stream)), "nanospec_token_logprob")
+
+
+def _grad(rows, d_grad):
+    """(address, type, stride) of a gradient tensor, checked against the rows it belongs to"""
+    if d_grad is None:
+        return None, F32, 0
+    kind, ld = _type_and_stride(d_grad)
+    if d_grad.shape[0] < rows.rows or d_grad.shape[1] < rows.V:
+        raise ValueError("the gradient has fewer rows or columns than the logits")
+    return d_grad.data_ptr(), kind, ld
+
+
+def nanospec_policy_loss(rows, d_old, d_ref, d_adv, d_weight, clip_low, clip_high, kl_beta, d_loss, d_row_loss, d_logprob, d_grad, d_workspace,
+                         workspace_bytes, grad_scale=1.0, stream=None):
+    g, kind, ld = _grad(rows, d_grad)
+    _check(lib().nanospec_policy_loss(rows, _ptr(d_old), _ptr(d_ref), _ptr(d_adv), _ptr(d_weight), clip_low, clip_high, kl_beta, _ptr(d_loss),
+                                      _ptr(d_row_loss), _ptr(d_logprob), g, kind, ld, grad_scale, _ptr(d_workspace), workspace_bytes,
+                                      _stream(stream)), "nanospec_policy_loss")
+
+
+def nanospec_preference_loss(rows, h_off, d_ref, d_weight, beta, smoothing, d_loss, d_margin, d_logprob, d_grad, d_workspace, workspace_bytes,
+                             grad_scale=1.0, stream=None):
+    """h_off: first row of every answer and the end of the last (2 pairs + 1 numbers), chosen and rejected in turn"""
+    off, op = _off(h_off)
+    if off.size % 2 == 0:
+        raise ValueError("h_off has a number more than there are answers, which come in pairs")
+    g, kind, ld = _grad(rows, d_grad)
+    _check(lib().nanospec_preference_loss(rows, op, off.size // 2, _ptr(d_ref), _ptr(d_weight), beta, smoothing, _ptr(d_loss), _ptr(d_margin),
+                                          _ptr(d_logprob), g, kind, ld, grad_scale, _ptr(d_workspace), workspace_bytes,
+                                          _stream(stream)), "nanospec_preference_loss")
 
 
 def nanospec_last_device_error(st, stream=None) -> int:

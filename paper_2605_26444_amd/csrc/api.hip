@@ -112,6 +112,40 @@ nanospec_status vocab_call(nanospec_state* st, const int32_t* d_new, const int32
   return NANOSPEC_OK;
 }
 
+bool aligned_to(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+// sizes of an 8-bit product: 16-byte pieces, int32 sums of products up to 127 * 127, 32-bit byte offsets
+bool i8_sizes_ok(int64_t rows, int32_t d) { return rows >= 1 && d >= 16 && d % 16 == 0 && d <= 133136 && rows * d <= 0xffffffffll; }
+
+nanospec_status head_i8(const int8_t* W, const float* W_scale, const void* H, const int32_t* ids, const int32_t* n_dev, int32_t cap, int32_t V, int32_t batch, int32_t M,
+                        int32_t d, int64_t ld, float* logits, void* ws, int64_t ws_bytes, void* stream) {
+  if (!aligned_to(W, 16) || !aligned_to(H, 16) || !aligned_to(ws, 256) || !i8_sizes_ok(V, d) || !i8_sizes_ok((int64_t)batch * M, d)) return NANOSPEC_EINVAL;
+  if (ws_bytes < head_i8_workspace_bytes(batch * M, d)) return NANOSPEC_ECAPACITY;
+  return launch_head_i8(W, W_scale, H, ids, n_dev, cap, V, batch, M, d, ld, logits, static_cast<char*>(ws), static_cast<hipStream_t>(stream)) == hipSuccess ? NANOSPEC_OK
+                                                                                                                                                   : NANOSPEC_EHIP;
+}
+
+// what a caller gave as rows of logits, for the kernels; without weights and with all rows counting
+nanospec_status logit_rows_of(const nanospec_logit_rows* in, const void* ws, int64_t ws_bytes, LogitRows* r) {
+  if (!in || !in->d_logits || !in->d_tokens || !ws || in->rows < 1 || in->V < 1 || in->V > (1 << 30) || in->ld < in->V || in->ld > (1ll << 60) / in->rows) return NANOSPEC_EINVAL;
+  if (in->type != NANOSPEC_F32 && in->type != NANOSPEC_BF16) return NANOSPEC_EINVAL;
+  if (!in->d_ids != !in->d_n || (in->d_ids && in->rows_per_list < 1) || !aligned_to(ws, 256)) return NANOSPEC_EINVAL;
+  if (ws_bytes < loss_workspace_bytes(in->rows, in->V)) return NANOSPEC_ECAPACITY;
+  *r = LogitRows{in->d_logits, in->d_tokens, in->d_ids, in->d_n, nullptr, in->ld, in->type, in->rows, in->V, in->d_ids ? in->rows_per_list : in->rows, 0, in->rows};
+  return NANOSPEC_OK;
+}
+
+// the gradient may lie on the logits exactly, not across them
+bool grad_ok(const LogitRows& r, const void* grad, int32_t type, int64_t ld) {
+  if (!grad) return true;
+  if ((type != NANOSPEC_F32 && type != NANOSPEC_BF16) || ld < r.V || ld > (1ll << 60) / r.rows) return false;
+  if (grad == r.z) return type == r.type && ld == r.ld;
+  const uintptr_t z0 = reinterpret_cast<uintptr_t>(r.z), g0 = reinterpret_cast<uintptr_t>(grad);
+  const uintptr_t z1 = z0 + ((uintptr_t)(r.rows - 1) * r.ld + r.V) * (r.type == NANOSPEC_F32 ? 4 : 2);
+  const uintptr_t g1 = g0 + ((uintptr_t)(r.rows - 1) * ld + r.V) * (type == NANOSPEC_F32 ? 4 : 2);
+  return g1 <= z0 || z1 <= g0;
+}
+
 }  // namespace
 
 extern "C" {
@@ -438,6 +472,73 @@ nanospec_status nanospec_dense_topk(const float* d_logits, int32_t V, int32_t M_
   hipError_t e = launch_topk(d_logits, V, nullptr, 0, nullptr, V, V, V, 1, M_total, k, d_out_ids, d_out_vals, false,
                              static_cast<char*>(d_workspace), workspace_bytes, static_cast<hipStream_t>(hip_stream));
   return e == hipSuccess ? NANOSPEC_OK : NANOSPEC_EHIP;
+}
+
+nanospec_status nanospec_quantize_rows(const void* d_X_bf16, int64_t rows, int32_t d, int8_t* d_Q, float* d_scale, void* hip_stream) {
+  if (!d_X_bf16 || !d_Q || !d_scale || !aligned_to(d_X_bf16, 16) || !aligned_to(d_Q, 16) || rows > 0xffffffffll || !i8_sizes_ok(rows, d)) return NANOSPEC_EINVAL;
+  return launch_quantize_rows(d_X_bf16, rows, d, d_Q, d_scale, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? NANOSPEC_OK : NANOSPEC_EHIP;
+}
+
+int64_t nanospec_head_i8_workspace(int32_t rows, int32_t d) { return i8_sizes_ok(rows, d) ? head_i8_workspace_bytes(rows, d) : -1; }
+
+nanospec_status nanospec_dense_head_i8(const int8_t* d_W_i8, const float* d_W_scale, const void* d_H_bf16, int32_t V, int32_t d, int32_t M_total, float* d_logits,
+                                       void* d_workspace, int64_t workspace_bytes, void* hip_stream) {
+  if (!d_W_i8 || !d_W_scale || !d_H_bf16 || !d_logits || !d_workspace || M_total < 1) return NANOSPEC_EINVAL;
+  if (ensure_device_configured() != hipSuccess) return NANOSPEC_EHIP;   // a flag test after the first call on the device
+  return head_i8(d_W_i8, d_W_scale, d_H_bf16, nullptr, nullptr, V, V, 1, M_total, d, V, d_logits, d_workspace, workspace_bytes, hip_stream);
+}
+
+nanospec_status nanospec_sparse_head_i8(nanospec_state* st, const int8_t* d_W_i8, const float* d_W_scale, const void* d_H_bf16, int32_t M, float* d_logits,
+                                        void* d_workspace, int64_t workspace_bytes, void* hip_stream) {
+  if (!st || !d_W_i8 || !d_W_scale || !d_H_bf16 || !d_logits || !d_workspace || M < 1 || wrong_device(st)) return NANOSPEC_EINVAL;
+  if (M > st->m_cap) return NANOSPEC_ECAPACITY;
+  return head_i8(d_W_i8, d_W_scale, d_H_bf16, st->vp.ids, st->vp.n, st->vp.cap, st->V, st->batch, M, st->d, st->vp.cap, d_logits, d_workspace, workspace_bytes, hip_stream);
+}
+
+int64_t nanospec_loss_workspace(int32_t rows, int32_t V) { return rows < 1 || V < 1 || V > (1 << 30) ? -1 : loss_workspace_bytes(rows, V); }
+
+nanospec_status nanospec_token_logprob(const nanospec_logit_rows* rows, float* d_logprob, void* d_workspace, int64_t workspace_bytes, void* hip_stream) {
+  LogitRows r;
+  if (!d_logprob) return NANOSPEC_EINVAL;
+  const nanospec_status rc = logit_rows_of(rows, d_workspace, workspace_bytes, &r);
+  if (rc != NANOSPEC_OK) return rc;
+  return launch_token_logprob(r, d_logprob, static_cast<char*>(d_workspace), static_cast<hipStream_t>(hip_stream)) == hipSuccess ? NANOSPEC_OK : NANOSPEC_EHIP;
+}
+
+nanospec_status nanospec_policy_loss(const nanospec_logit_rows* rows, const float* d_old, const float* d_ref, const float* d_adv, const float* d_weight, float clip_low,
+                                     float clip_high, float kl_beta, float* d_loss, float* d_row_loss, float* d_logprob, void* d_grad, int32_t grad_type, int64_t ld_grad,
+                                     float grad_scale, void* d_workspace, int64_t workspace_bytes, void* hip_stream) {
+  LogitRows r;
+  if (!d_old || !d_adv || !d_loss || !(clip_low >= 0.f) || !(clip_high >= 0.f) || kl_beta != kl_beta || grad_scale != grad_scale || (kl_beta != 0.f && !d_ref))
+    return NANOSPEC_EINVAL;
+  const nanospec_status rc = logit_rows_of(rows, d_workspace, workspace_bytes, &r);
+  if (rc != NANOSPEC_OK) return rc;
+  if (!grad_ok(r, d_grad, grad_type, ld_grad)) return NANOSPEC_EINVAL;
+  r.weight = d_weight;
+  const PolicyArgs a{d_old, kl_beta != 0.f ? d_ref : nullptr, d_adv, clip_low, clip_high, kl_beta, grad_scale, d_loss, d_row_loss, d_logprob};
+  return launch_policy_loss(r, a, d_grad, grad_type, ld_grad, static_cast<char*>(d_workspace), static_cast<hipStream_t>(hip_stream)) == hipSuccess ? NANOSPEC_OK
+                                                                                                                                                    : NANOSPEC_EHIP;
+}
+
+nanospec_status nanospec_preference_loss(const nanospec_logit_rows* rows, const int32_t* h_off, int32_t pairs, const float* d_ref, const float* d_weight, float beta,
+                                         float smoothing, float* d_loss, float* d_margin, float* d_logprob, void* d_grad, int32_t grad_type, int64_t ld_grad,
+                                         float grad_scale, void* d_workspace, int64_t workspace_bytes, void* hip_stream) {
+  LogitRows r;
+  if (!h_off || !d_loss || pairs < 1 || beta != beta || !(smoothing >= 0.f) || !(smoothing <= 1.f) || grad_scale != grad_scale) return NANOSPEC_EINVAL;
+  nanospec_status rc = logit_rows_of(rows, d_workspace, workspace_bytes, &r);
+  if (rc != NANOSPEC_OK) return rc;
+  if (pairs > NANOSPEC_MAX_BATCH / 2) return NANOSPEC_ECAPACITY;
+  Offsets off;
+  bool any;
+  rc = offsets_to_arg(h_off, 2 * pairs, &off, -1, &any);
+  if (rc != NANOSPEC_OK) return rc;
+  if (off.v[2 * pairs] > r.rows || !grad_ok(r, d_grad, grad_type, ld_grad)) return NANOSPEC_EINVAL;
+  r.weight = d_weight;
+  r.first = off.v[0];
+  r.last = off.v[2 * pairs];
+  const PairArgs a{d_ref, pairs, beta, smoothing, grad_scale, d_loss, d_margin, d_logprob};
+  return launch_preference_loss(r, a, off, d_grad, grad_type, ld_grad, static_cast<char*>(d_workspace), static_cast<hipStream_t>(hip_stream)) == hipSuccess ? NANOSPEC_OK
+                                                                                                                                                             : NANOSPEC_EHIP;
 }
 
 nanospec_status nanospec_calib_stream_read(const void* d_buf, int64_t bytes, void* d_sink, void* hip_stream) {

@@ -127,6 +127,12 @@ inline WideShape wide_shape(int32_t M, int32_t d, int32_t batch, int32_t cap_row
   return d % 64 == 0 && aligned ? kWideGemm : kWide256x256;
 }
 
+// The 8-bit head's: as many bytes a step hold twice the columns.  256 x 256 blocks with the scales do not fit LDS, so d that is no multiple of 128 takes 256 x 128.
+inline WideShape i8_shape(int32_t M, int32_t d, int32_t batch, int32_t cap_rows, bool dense) {
+  const WideShape s = wide_shape(M, d / 2, batch, cap_rows, dense, d % 128 == 0);
+  return s == kWide256x256 ? kWide256x128 : s;
+}
+
 // Sequences hold many of the same rows, and a die's L2 sees a row again only if the sequences that hold it run there at the
 // same time: for few hidden rows each die takes one eighth of every list (64 sequences of 2300 rows, M = 8: 135 -> 130.5 us, 32: 79
 // -> 73.5, 16: 47 -> 43; 8, M = 16: 31.1 -> 29.4), but not where the hidden rows of all sequences, which every die then needs, are as

@@ -49,6 +49,55 @@ __device__ __forceinline__ void lds_fetch16(uint32_t lds, const void* base, uint
 }
 #pragma clang diagnostic pop
 
+// A row in 8 bits (quant.hip): a = max |x|, scale = a / 127, q = 127 x / a to the nearest integer, ties to even.
+// Computed on x and a times a power of two that leaves a in [0.5, 1), in two factors, so that nothing overflows and a is no denormal; what
+// the factors lose of a tiny x rounds to q = 0 either way.  127 x of a bf16 x is exact in fp32 (15 bits) and so is the decision: the
+// quotient of a 15-bit by an 8-bit number is a tie or at least 2^-9 away from one, and the quotient here -- by the reciprocal, with one
+// correction -- is exact if it is a tie and 2^-16 off at most otherwise.  So q is what exact arithmetic gives.
+struct I8Row {
+  float p, p127, a, r;
+  uint32_t mask;       // 0: a row of zeros, or one with an infinity or a NaN: all q are 0
+  float scale;
+};
+
+// top: the largest magnitude's bits (of all the row's numbers, signs cleared: an infinity or a NaN is larger than any number)
+__device__ __forceinline__ I8Row i8_row(uint32_t top_bits) {
+  I8Row k;
+  const bool bad = top_bits >= 0x7f800000u;
+  const float top = __uint_as_float(top_bits);
+  const int e = bad || top_bits == 0 ? 0 : __builtin_amdgcn_frexp_expf(top);
+  const int e1 = e >> 1, e2 = e - e1;
+  k.p = __uint_as_float((uint32_t)(127 - e1) << 23);
+  k.p127 = 127.f * __uint_as_float((uint32_t)(127 - e2) << 23);
+  k.mask = bad || top_bits == 0 ? 0u : 0xffffffffu;
+  k.a = k.mask ? top * k.p * __uint_as_float((uint32_t)(127 - e2) << 23) : 1.f;
+  k.r = 1.f / k.a;
+  k.scale = bad ? __builtin_nanf("") : top / 127.f;
+  return k;
+}
+
+// q of one number in the low byte: adding 1.5 * 2^23 rounds to an integer
+__device__ __forceinline__ uint32_t i8_round(const I8Row& k, uint32_t x_bits) {
+  const float n = __uint_as_float(x_bits & k.mask) * k.p * k.p127, q = n * k.r;
+  return __float_as_uint(fmaf(fmaf(-q, k.a, n), k.r, q) + 12582912.f);
+}
+
+// four numbers of two bf16 pairs
+__device__ __forceinline__ uint32_t i8_round4(const I8Row& k, uint32_t x01, uint32_t x23) {
+  const uint32_t a = i8_round(k, x01 << 16), b = i8_round(k, x01 & 0xffff0000u), c = i8_round(k, x23 << 16), d = i8_round(k, x23 & 0xffff0000u);
+  return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400u), __builtin_amdgcn_perm(b, a, 0x0c0c0400u), 0x05040100u);
+}
+
+// largest magnitude of eight bf16, as the bits of an fp32 with the sign cleared
+__device__ __forceinline__ uint32_t bf16_top(uint32_t top, uint32_t x) {
+  const uint32_t lo = (x << 16) & 0x7fff0000u, hi = x & 0x7fff0000u;
+  const uint32_t m = lo > hi ? lo : hi;
+  return m > top ? m : top;
+}
+
+// A logit of the 8-bit heads: the integer sum rounded to fp32, then the two scales' product.  All kernels round in these places.
+__device__ __forceinline__ float i8_logit(int sum, float w_scale, float h_scale) { return (float)sum * (w_scale * h_scale); }
+
 // Per-sequence offsets travel by value in the kernel argument block (no H2D copy, graph-safe).
 struct Offsets {
   int32_t v[NANOSPEC_MAX_BATCH + 1];
@@ -95,6 +144,40 @@ struct UnionPtrs {
   int32_t* head_n;        // [batch]
   int32_t* head_shared_n; // [groups] as shared_n, or 0
   int32_t shared_cap, min_share;
+};
+
+// Rows of logits with a token each (nanospec_logit_rows, checked), the rows that count: first <= row < last, weight not zero.
+struct LogitRows {
+  const void* z;
+  const int32_t* tokens;
+  const int32_t* ids;     // ascending ids of the columns [..][V], or null: column = id
+  const int32_t* n;       // live columns of each list
+  const float* weight;    // [rows], or null: 1
+  int64_t ld;
+  int32_t type, rows, V, per_list, first, last;
+};
+
+struct RowCut {
+  int32_t pieces, span;   // pieces of a row, columns of a piece
+};
+
+struct PolicyArgs {
+  const float* old;
+  const float* ref;       // may be null
+  const float* adv;
+  float clip_low, clip_high, beta, grad_scale;
+  float* loss;            // [1]
+  float* row_loss;        // [rows], may be null
+  float* logprob;         // [rows], may be null
+};
+
+struct PairArgs {
+  const float* ref;       // may be null
+  int32_t pairs;
+  float beta, smoothing, grad_scale;
+  float* loss;            // [1]
+  float* margin;          // [pairs], may be null
+  float* logprob;         // [rows], may be null
 };
 
 }  // namespace nanospec
@@ -150,6 +233,8 @@ hipError_t launch_head_wide_shared(const void* W, const void* H, const int32_t* 
                                    int32_t rows_total, int32_t seq_rows, int32_t d, int64_t ld, float* logits, const int32_t* opos,
                                    int64_t opos_stride, hipStream_t s);
 hipError_t wide_configure_device();
+hipError_t launch_head_wide_i8(const int8_t* W, const float* W_scale, const int8_t* H, const float* H_scale, const int32_t* ids, const int32_t* n_dev, int32_t cap_rows,
+                               int32_t V, int32_t batch, int32_t M, int32_t d, int64_t ld, float* logits, hipStream_t s);
 hipError_t launch_head_wide(const void* W, const void* H, const int32_t* ids, const int32_t* n_dev, int32_t n_fixed, int32_t cap_rows,
                             int32_t V, int32_t batch, int32_t M, int32_t d, int64_t ld, int64_t ids_stride, float* logits,
                             const int32_t* opos, hipStream_t s);
@@ -174,6 +259,18 @@ int64_t topk_workspace_bytes(int32_t cap, int32_t rows, int32_t k);
 hipError_t launch_topk(const float* logits, int64_t ld, const int32_t* ids, int64_t ids_stride, const int32_t* n_dev,
                        int32_t n_fixed, int32_t cap, int64_t expected /* see topk_expected */, int32_t batch, int32_t M, int32_t k,
                        int32_t* out_ids, float* out_vals, bool logprob, char* ws, int64_t ws_bytes, hipStream_t s);
+
+// quant.hip: rows in 8 bits, and the heads on them
+int64_t head_i8_workspace_bytes(int32_t rows, int32_t d);
+hipError_t launch_quantize_rows(const void* X, int64_t rows, int32_t d, int8_t* q, float* scale, hipStream_t s);
+hipError_t launch_head_i8(const int8_t* W, const float* W_scale, const void* H, const int32_t* ids, const int32_t* n_dev, int32_t cap_rows, int32_t V, int32_t batch,
+                          int32_t M, int32_t d, int64_t ld, float* logits, char* ws, hipStream_t s);
+
+// loss.hip
+int64_t loss_workspace_bytes(int32_t rows, int32_t V);
+hipError_t launch_token_logprob(const LogitRows& r, float* logprob, char* ws, hipStream_t s);
+hipError_t launch_policy_loss(const LogitRows& r, const PolicyArgs& a, void* grad, int32_t grad_type, int64_t ld_grad, char* ws, hipStream_t s);
+hipError_t launch_preference_loss(const LogitRows& r, const PairArgs& a, const Offsets& off, void* grad, int32_t grad_type, int64_t ld_grad, char* ws, hipStream_t s);
 
 // packed.hip
 hipError_t packed_configure_device();

@@ -1,0 +1,478 @@
+// Log-probabilities of given tokens, and the two losses that a draft (or a policy) is trained with on the logits of a head, with the
+// gradient of those logits.
+//
+//   log p(a)  = (z_a - max z) - log sum_j exp(z_j - max z)
+//   policy      r = exp(log p - old), row = -min(r A, clip(r, 1 - lo, 1 + hi) A) + beta (exp(ref - log p) - (ref - log p) - 1), L = sum w row
+//   preference  margin = beta (S_chosen - S_rejected), S = sum of w (log p - ref) over an answer's rows,
+//               pair = -(1 - e) log sigma(margin) - e log sigma(-margin), L = mean over the pairs
+//   gradient    dL/dz_j = c ([j == a] - p_j) with c = dL/d(log p) of the row
+//
+// Everything but the two passes over the logits is a few numbers a row.  So: rows_stats_kernel reads each row once (running maximum and
+// sum, the row cut into pieces where rows are few), one workgroup turns the pieces into log-probabilities, losses and a coefficient
+// per row (in 64 bits, sums in a fixed order: the result is reproducible bit for bit), rows_grad_kernel reads the logits again and writes the gradient.
+#include "common.h"
+
+namespace nanospec {
+
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));           // rows start at any element: 16-byte loads at its alignment
+typedef uint16_t u16x8_any __attribute__((ext_vector_type(8), aligned(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8_any __attribute__((ext_vector_type(8), aligned(2)));
+
+constexpr int kRowThreads = 256;
+constexpr float kLog2e = 1.44269504088896340736f;
+
+__device__ __forceinline__ float exp_neg(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }   // x <= 0: the relative error is 2^-24 |x| at most beside the instruction's
+
+template <typename T>
+struct Vec;
+template <>
+struct Vec<float> {
+  static constexpr int N = 4;
+  static __device__ __forceinline__ void load(const float* p, float (&x)[N]) {
+    const f32x4_any v = *reinterpret_cast<const f32x4_any*>(p);
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = v[i];
+  }
+  static __device__ __forceinline__ float one(const float* p) { return *p; }
+};
+template <>
+struct Vec<uint16_t> {
+  static constexpr int N = 8;
+  static __device__ __forceinline__ void load(const uint16_t* p, float (&x)[N]) {
+    const u16x8_any v = *reinterpret_cast<const u16x8_any*>(p);
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = __uint_as_float((uint32_t)v[i] << 16);
+  }
+  static __device__ __forceinline__ float one(const uint16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
+};
+
+template <int N>
+__device__ __forceinline__ void store_vec(float* p, const float (&x)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; i += 4) *reinterpret_cast<f32x4_any*>(p + i) = f32x4_any{x[i], x[i + 1], x[i + 2], x[i + 3]};
+}
+template <int N>
+__device__ __forceinline__ void store_vec(uint16_t* p, const float (&x)[N]) {       // rounded to nearest even, the only rounding of the gradient
+  if constexpr (N == 8) {
+    bf16x8 v;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (__bf16)x[i];
+    *reinterpret_cast<bf16x8_any*>(p) = v;
+  } else {
+    typedef __bf16 bf16x4_any __attribute__((ext_vector_type(4), aligned(2)));
+    bf16x4_any v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = (__bf16)x[i];
+    *reinterpret_cast<bf16x4_any*>(p) = v;
+  }
+}
+__device__ __forceinline__ void store_one(float* p, float x) { *p = x; }
+__device__ __forceinline__ void store_one(uint16_t* p, float x) { *p = __builtin_bit_cast(uint16_t, (__bf16)x); }
+
+// a running maximum and the sum of exp(z - maximum); {-inf, 0} is nothing.  A NaN, or +inf, makes the sum NaN.
+struct Stat {
+  float m, s;
+};
+
+__device__ __forceinline__ float finite_or_zero(float m) { return m == -INFINITY ? 0.f : m; }   // rows of -inf: exp(-inf - 0) = 0
+
+__device__ __forceinline__ Stat join(Stat a, Stat b) {
+  const float m = fmaxf(a.m, b.m), mm = finite_or_zero(m);
+  return Stat{m, a.s * exp_neg(a.m - mm) + b.s * exp_neg(b.m - mm)};
+}
+
+template <int N>
+__device__ __forceinline__ void take(Stat& t, const float (&x)[N]) {
+  float top = x[0];
+#pragma unroll
+  for (int i = 1; i < N; ++i) top = fmaxf(top, x[i]);
+  const float m = fmaxf(t.m, top), mm = finite_or_zero(m);
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) s += exp_neg(x[i] - mm);
+  t.s = t.s * exp_neg(t.m - mm) + s;
+  t.m = m;
+}
+
+__device__ __forceinline__ Stat wave_join(Stat t) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) t = join(t, Stat{__shfl_xor(t.m, o), __shfl_xor(t.s, o)});
+  return t;
+}
+
+// a token's column (-1: none) and logit (-inf: none)
+struct Place {
+  float z;
+  int col;
+};
+
+// -inf where the token has no column or its logit is -inf; both maximum and logit are exact, so only the sum carries a rounding
+__device__ __forceinline__ double log_probability(const Place& a, const Stat& t) {
+  return a.z == -INFINITY ? -INFINITY : ((double)a.z - (double)t.m) - log((double)t.s);
+}
+
+// column of a row's token: the token itself, or its place in the ascending list; -1 if it has none.  One wavefront, every lane gets it.
+__device__ __forceinline__ int token_column(const LogitRows& r, int row, int n) {
+  const int t = r.tokens[row];
+  if (!r.ids) return t >= 0 && t < n ? t : -1;
+  const int32_t* ids = r.ids + (int64_t)(row / r.per_list) * r.V;
+  const int lane = threadIdx.x & 63;
+  int lo = 0, len = n;                                     // the places that may still hold it
+  while (len > 0) {
+    const int step = (len + 63) >> 6, at = lo + lane * step;
+    const bool in = at < lo + len;
+    const int v = in ? ids[at] : 0;
+    const uint64_t hit = __ballot(in && v == t);
+    if (hit) return lo + (__ffsll((unsigned long long)hit) - 1) * step;
+    const uint64_t below = __ballot(in && v < t);
+    if (!below || step == 1) return -1;
+    const int k = __popcll(below) - 1, end = lo + len;     // behind the last probe below it
+    lo += k * step + 1;
+    len = (step - 1 < end - lo) ? step - 1 : end - lo;
+  }
+  return -1;
+}
+
+__device__ __forceinline__ int row_columns(const LogitRows& r, int row) {
+  if (!r.n) return r.V;
+  const int n = r.n[row / r.per_list];
+  return n < r.V ? n : r.V;
+}
+
+__device__ __forceinline__ bool row_counts(const LogitRows& r, int row) {
+  return row >= r.first && row < r.last && (!r.weight || r.weight[row] != 0.f);
+}
+
+// Piece `blockIdx.x % pieces` of row `blockIdx.x / pieces`: maximum and sum of its columns to part[], and the token's column and logit, from
+// the workgroup that has the row's first columns, to at[].  Rows that do not count are not read.
+template <typename T>
+__global__ __launch_bounds__(kRowThreads) void rows_stats_kernel(const LogitRows r, int pieces, int span, Stat* __restrict__ part, Place* __restrict__ at,
+                                                                 float* __restrict__ logprob) {
+  constexpr int N = Vec<T>::N, U = 16 / N;
+  const int row = blockIdx.x / pieces, piece = blockIdx.x - row * pieces, tid = threadIdx.x, w = tid >> 6;
+  if (!row_counts(r, row)) return;
+  const T* z = static_cast<const T*>(r.z) + (int64_t)row * r.ld;
+  const int n = row_columns(r, row);
+  const int c0 = piece * span, c1 = c0 + span < n ? c0 + span : n;
+  Place a{-INFINITY, -1};
+  if (piece == 0 && w == 0) {
+    a.col = token_column(r, row, n);
+    if (a.col >= 0) a.z = Vec<T>::one(z + a.col);
+  }
+  Stat t{-INFINITY, 0.f};
+  int c = c0;
+  for (; c + kRowThreads * N * U <= c1; c += kRowThreads * N * U) {
+    float x[U * N];
+#pragma unroll
+    for (int u = 0; u < U; ++u) Vec<T>::load(z + c + (u * kRowThreads + tid) * N, *reinterpret_cast<float(*)[N]>(&x[u * N]));
+    take(t, x);
+  }
+  for (c += tid * N; c < c1; c += kRowThreads * N) {
+    float x[N];
+    if (c + N <= c1) {
+      Vec<T>::load(z + c, x);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] = c + i < c1 ? Vec<T>::one(z + c + i) : -INFINITY;
+    }
+    take(t, x);
+  }
+  t = wave_join(t);
+  __shared__ Stat red[kRowThreads / 64];
+  if ((tid & 63) == 0) red[w] = t;
+  __syncthreads();
+  if (tid) return;
+#pragma unroll
+  for (int i = 1; i < kRowThreads / 64; ++i) t = join(t, red[i]);
+  if (logprob) {                                           // one piece and nothing else asked for
+    logprob[row] = (float)log_probability(a, t);
+    return;
+  }
+  part[(int64_t)row * pieces + piece] = t;
+  if (piece == 0) at[row] = a;
+}
+
+struct RowResult {
+  Stat t;
+  double lp;
+  int col;
+  bool has;          // the token has a probability: exp(lp) is not zero in 64 bits
+};
+
+__device__ __forceinline__ RowResult finish_row(int row, int pieces, const Stat* __restrict__ part, const Place* __restrict__ at) {
+  RowResult q;
+  const Place a = at[row];
+  q.t = part[(int64_t)row * pieces];
+  for (int i = 1; i < pieces; ++i) q.t = join(q.t, part[(int64_t)row * pieces + i]);
+  q.lp = log_probability(a, q.t);
+  q.col = a.col;
+  q.has = !(q.lp < -745.0);
+  return q;
+}
+
+__global__ __launch_bounds__(256) void rows_logprob_kernel(int rows, int pieces, const Stat* __restrict__ part, const Place* __restrict__ at, float* __restrict__ logprob) {
+  const int row = blockIdx.x * 256 + threadIdx.x;
+  if (row < rows) logprob[row] = (float)finish_row(row, pieces, part, at).lp;
+}
+
+// sum over a workgroup of 1024 in a fixed order, in thread 0
+__device__ __forceinline__ double block_sum(double x, double* red) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) x += __shfl_down(x, o);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
+  __syncthreads();
+  double s = 0;
+  if (threadIdx.x == 0)
+    for (int i = 0; i < 16; ++i) s += red[i];
+  return s;
+}
+
+// what the gradient pass needs of a row: the maximum, -c / sum and c; c == 0: the row's gradient is zero
+struct RowCoef {
+  float m, scale, c;
+  int col;
+};
+
+__device__ __forceinline__ RowCoef coef_of(const Stat& t, int col, double c, float grad_scale) {
+  return RowCoef{t.m, (float)(-(c * grad_scale) / (double)t.s), (float)(c * grad_scale), col};
+}
+
+__global__ __launch_bounds__(1024) void policy_rows_kernel(const LogitRows r, int pieces, const Stat* __restrict__ part, const Place* __restrict__ at, const PolicyArgs a,
+                                                           RowCoef* __restrict__ coef) {
+  __shared__ double red[16];
+  double sum = 0;
+  for (int row = threadIdx.x; row < r.rows; row += 1024) {
+    float lp_out = 0.f, loss_out = 0.f;
+    RowCoef k{0.f, 0.f, 0.f, -1};
+    if (row_counts(r, row)) {
+      const RowResult q = finish_row(row, pieces, part, at);
+      lp_out = (float)q.lp;
+      if (q.has) {
+        const double w = r.weight ? (double)r.weight[row] : 1.0, adv = a.adv[row];
+        const double ratio = exp(q.lp - (double)a.old[row]);
+        const double lo = 1.0 - (double)a.clip_low, hi = 1.0 + (double)a.clip_high;
+        const double held = (ratio < lo ? lo : ratio > hi ? hi : ratio) * adv, free = ratio * adv;
+        double loss = -(free <= held ? free : held), c = free <= held ? -free : 0.0;
+        if (free != free) loss = c = free;                 // NaN stays NaN
+        if (a.ref) {
+          const double gap = (double)a.ref[row] - q.lp, e = exp(gap);
+          loss += (double)a.beta * (e - gap - 1.0);
+          c += (double)a.beta * (1.0 - e);
+        }
+        loss_out = (float)loss;
+        sum += w * loss;
+        k = coef_of(q.t, q.col, w * c, a.grad_scale);
+      }
+    }
+    if (a.row_loss) a.row_loss[row] = loss_out;
+    if (a.logprob) a.logprob[row] = lp_out;
+    if (coef) coef[row] = k;
+  }
+  sum = block_sum(sum, red);
+  if (threadIdx.x == 0) a.loss[0] = (float)sum;
+}
+
+// one workgroup; the answers' first rows travel by value
+__global__ __launch_bounds__(1024) void pair_rows_kernel(const LogitRows r, int pieces, const Stat* __restrict__ part, const Place* __restrict__ at, const PairArgs a, const Offsets off,
+                                                         double* __restrict__ term, RowCoef* __restrict__ coef) {
+  __shared__ double red[16], sums[NANOSPEC_MAX_BATCH];
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  for (int row = tid; row < r.rows; row += 1024) {
+    float lp_out = 0.f;
+    double t = 0;
+    RowCoef k{0.f, 0.f, 0.f, -1};
+    if (row_counts(r, row)) {
+      const RowResult q = finish_row(row, pieces, part, at);
+      lp_out = (float)q.lp;
+      if (q.has) {
+        const double wt = r.weight ? (double)r.weight[row] : 1.0;
+        t = wt * (q.lp - (a.ref ? (double)a.ref[row] : 0.0));
+        k = RowCoef{q.t.m, q.t.s, (float)wt, q.col};
+      }
+    }
+    if (a.logprob) a.logprob[row] = lp_out;
+    term[row] = t;
+    if (coef) coef[row] = k;
+  }
+  __threadfence_block();
+  __syncthreads();
+  for (int q = w; q < 2 * a.pairs; q += 16) {              // a wavefront an answer
+    double s = 0;
+    for (int row = off.v[q] + lane; row < off.v[q + 1]; row += 64) s += term[row];
+#pragma unroll
+    for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
+    if (lane == 0) sums[q] = s;
+  }
+  __syncthreads();
+  double loss = 0, slope = 0;
+  if (tid < a.pairs) {
+    const double margin = (double)a.beta * (sums[2 * tid] - sums[2 * tid + 1]), e = (double)a.smoothing;
+    const double less = log1p(exp(-fabs(margin)));         // log(1 + exp(-m)) = max(-m, 0) + less
+    loss = (1.0 - e) * (fmax(-margin, 0.0) + less) + e * (fmax(margin, 0.0) + less);
+    if (margin != margin) loss = margin;
+    const double up = 1.0 / (1.0 + exp(margin)), down = 1.0 / (1.0 + exp(-margin));   // sigma(-m), sigma(m)
+    slope = ((1.0 - e) * -up + e * down) * (double)a.beta / a.pairs;
+    if (a.margin) a.margin[tid] = (float)margin;
+  }
+  __syncthreads();
+  if (tid < a.pairs) sums[tid] = slope;
+  loss = block_sum(loss, red);                             // and a barrier behind sums[]
+  if (tid == 0) a.loss[0] = (float)(loss / a.pairs);
+  if (!coef) return;
+  for (int row = tid; row < r.rows; row += 1024) {
+    const RowCoef k = coef[row];                           // written by this thread
+    RowCoef out{0.f, 0.f, 0.f, -1};
+    if (k.col >= 0) {
+      int lo = 0, hi = 2 * a.pairs;                        // the answer that holds the row: off[lo] <= row < off[lo + 1]
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (off.v[mid] <= row) lo = mid;
+        else hi = mid;
+      }
+      out = coef_of(Stat{k.m, k.scale}, k.col, (lo & 1 ? -1.0 : 1.0) * sums[lo >> 1] * (double)k.c, a.grad_scale);
+    }
+    coef[row] = out;
+  }
+}
+
+// dL/dz of piece `blockIdx.x % pieces` of a row
+template <typename T, typename G>
+__global__ __launch_bounds__(kRowThreads) void rows_grad_kernel(const LogitRows r, int pieces, int span, const RowCoef* __restrict__ coef, G* __restrict__ grad, int64_t ld_grad) {
+  constexpr int N = Vec<T>::N, U = 16 / N;
+  const int row = blockIdx.x / pieces, piece = blockIdx.x - row * pieces, tid = threadIdx.x;
+  const T* z = static_cast<const T*>(r.z) + (int64_t)row * r.ld;     // may be the gradient's own memory: every element is read by the thread that writes it
+  G* g = grad + (int64_t)row * ld_grad;
+  const RowCoef k = coef[row];
+  const int n = row_columns(r, row);
+  const int c0 = piece * span, c1 = c0 + span < n ? c0 + span : n;
+  if (k.c == 0.f) {
+    for (int c = c0 + tid * N; c < c1; c += kRowThreads * N) {
+      const float x[N] = {};
+      if (c + N <= c1) store_vec(g + c, x);
+      else
+        for (int i = c; i < c1; ++i) store_one(g + i, 0.f);
+    }
+    return;
+  }
+  auto one = [&](float x, int c) {
+    const float p = k.scale * exp_neg(x - k.m);
+    return c == k.col ? p + k.c : p;
+  };
+  int c = c0;
+  for (; c + kRowThreads * N * U <= c1; c += kRowThreads * N * U) {
+    float x[U][N];
+#pragma unroll
+    for (int u = 0; u < U; ++u) Vec<T>::load(z + c + (u * kRowThreads + tid) * N, x[u]);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int b = c + (u * kRowThreads + tid) * N;
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[u][i] = one(x[u][i], b + i);
+      store_vec(g + b, x[u]);
+    }
+  }
+  for (c += tid * N; c < c1; c += kRowThreads * N) {
+    if (c + N <= c1) {
+      float x[N];
+      Vec<T>::load(z + c, x);
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] = one(x[i], c + i);
+      store_vec(g + c, x);
+    } else {
+      for (int i = c; i < c1; ++i) store_one(g + i, one(Vec<T>::one(z + i), i));
+    }
+  }
+}
+
+// ---- host --------------------------------------------------------------------------------------------------------
+
+// Rows cut into pieces until there are 2048 workgroups (eight a compute unit), of no less than 4096 columns, a multiple of what a pass of a workgroup takes.
+static RowCut row_cut(int32_t rows, int32_t V) {
+  int64_t pieces = (2048 + rows - 1) / rows;
+  const int64_t most = (V + 4095) / 4096;
+  if (pieces > most) pieces = most;
+  const int64_t span = ((V + pieces - 1) / pieces + 4095) / 4096 * 4096;
+  return RowCut{(int32_t)((V + span - 1) / span), (int32_t)(span < V ? span : V)};
+}
+
+static int64_t up256(int64_t x) { return (x + 255) / 256 * 256; }
+
+struct LossSpace {
+  Stat* part;
+  Place* at;
+  RowCoef* coef;
+  double* term;
+};
+
+static LossSpace loss_space(char* p, int32_t rows, int32_t V) {
+  LossSpace s;
+  s.part = reinterpret_cast<Stat*>(p);
+  p += up256((int64_t)rows * row_cut(rows, V).pieces * sizeof(Stat));
+  s.coef = reinterpret_cast<RowCoef*>(p);
+  p += up256((int64_t)rows * sizeof(RowCoef));
+  s.term = reinterpret_cast<double*>(p);
+  p += up256((int64_t)rows * sizeof(double));
+  s.at = reinterpret_cast<Place*>(p);
+  return s;
+}
+
+int64_t loss_workspace_bytes(int32_t rows, int32_t V) {
+  return up256((int64_t)rows * row_cut(rows, V).pieces * sizeof(Stat)) + up256((int64_t)rows * sizeof(RowCoef)) + up256((int64_t)rows * sizeof(double)) +
+         up256((int64_t)rows * sizeof(Place));
+}
+
+static hipError_t run_stats(const LogitRows& r, const LossSpace& s, float* logprob, hipStream_t stream) {
+  const RowCut cut = row_cut(r.rows, r.V);
+  const int64_t grid = (int64_t)r.rows * cut.pieces;
+  if (grid > 0x7fffffff) return hipErrorInvalidValue;
+  if (r.type == NANOSPEC_F32)
+    rows_stats_kernel<float><<<dim3((unsigned)grid), kRowThreads, 0, stream>>>(r, cut.pieces, cut.span, s.part, s.at, logprob);
+  else
+    rows_stats_kernel<uint16_t><<<dim3((unsigned)grid), kRowThreads, 0, stream>>>(r, cut.pieces, cut.span, s.part, s.at, logprob);
+  return hipGetLastError();
+}
+
+static hipError_t run_grad(const LogitRows& r, const LossSpace& s, void* grad, int32_t type, int64_t ld, hipStream_t stream) {
+  const RowCut cut = row_cut(r.rows, r.V);
+  const unsigned grid = (unsigned)((int64_t)r.rows * cut.pieces);
+#define NS_GRAD(T, G) rows_grad_kernel<T, G><<<dim3(grid), kRowThreads, 0, stream>>>(r, cut.pieces, cut.span, s.coef, static_cast<G*>(grad), ld)
+  if (r.type == NANOSPEC_F32) {
+    if (type == NANOSPEC_F32) NS_GRAD(float, float);
+    else NS_GRAD(float, uint16_t);
+  } else {
+    if (type == NANOSPEC_F32) NS_GRAD(uint16_t, float);
+    else NS_GRAD(uint16_t, uint16_t);
+  }
+#undef NS_GRAD
+  return hipGetLastError();
+}
+
+hipError_t launch_token_logprob(const LogitRows& r, float* logprob, char* ws, hipStream_t stream) {
+  const LossSpace s = loss_space(ws, r.rows, r.V);
+  const int pieces = row_cut(r.rows, r.V).pieces;
+  hipError_t e = run_stats(r, s, pieces == 1 ? logprob : nullptr, stream);
+  if (e != hipSuccess || pieces == 1) return e;
+  rows_logprob_kernel<<<dim3((unsigned)((r.rows + 255) / 256)), 256, 0, stream>>>(r.rows, pieces, s.part, s.at, logprob);
+  return hipGetLastError();
+}
+
+hipError_t launch_policy_loss(const LogitRows& r, const PolicyArgs& a, void* grad, int32_t grad_type, int64_t ld_grad, char* ws, hipStream_t stream) {
+  const LossSpace s = loss_space(ws, r.rows, r.V);
+  hipError_t e = run_stats(r, s, nullptr, stream);
+  if (e != hipSuccess) return e;
+  policy_rows_kernel<<<dim3(1), 1024, 0, stream>>>(r, row_cut(r.rows, r.V).pieces, s.part, s.at, a, grad ? s.coef : nullptr);
+  e = hipGetLastError();
+  return e == hipSuccess && grad ? run_grad(r, s, grad, grad_type, ld_grad, stream) : e;
+}
+
+hipError_t launch_preference_loss(const LogitRows& r, const PairArgs& a, const Offsets& off, void* grad, int32_t grad_type, int64_t ld_grad, char* ws, hipStream_t stream) {
+  const LossSpace s = loss_space(ws, r.rows, r.V);
+  hipError_t e = run_stats(r, s, nullptr, stream);
+  if (e != hipSuccess) return e;
+  pair_rows_kernel<<<dim3(1), 1024, 0, stream>>>(r, row_cut(r.rows, r.V).pieces, s.part, s.at, a, off, s.term, grad ? s.coef : nullptr);
+  e = hipGetLastError();
+  return e == hipSuccess && grad ? run_grad(r, s, grad, grad_type, ld_grad, stream) : e;
+}
+
+}  // namespace nanospec

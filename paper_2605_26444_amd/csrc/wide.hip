@@ -17,6 +17,39 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef f32x4 f32x4_u __attribute__((aligned(4)));   // global memory takes 16-byte stores at any 4-byte address
 
+// What is multiplied.  Operands are 16-byte pieces of rows whichever it is: 8 numbers of bf16, or 16 of int8, in which case
+// the kernels' d counts pairs of columns.  Both instructions take a piece a lane of each operand and leave their results in the same places.
+struct ProductBf16 {
+  typedef bf16x8 Piece;
+  typedef f32x4 Acc;
+  static constexpr bool kScaled = false;
+  static __device__ __forceinline__ Acc mul(Piece a, Piece b, Acc c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+  __device__ __forceinline__ float w_scale(int64_t) const { return 1.f; }
+  __device__ __forceinline__ float h_scale(int64_t) const { return 1.f; }
+};
+
+// Integer sums, rounded once to fp32 and multiplied with the scales of the row and of the hidden row (quant.hip): the same logits from every kernel.
+struct ProductI8 {
+  typedef int32_t Piece __attribute__((ext_vector_type(4)));
+  typedef Piece Acc;
+  static constexpr bool kScaled = true;
+  const float* w;      // [V]
+  const float* h;      // [batch * M]
+  static __device__ __forceinline__ Acc mul(Piece a, Piece b, Acc c) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0); }
+  __device__ __forceinline__ float w_scale(int64_t i) const { return w[i]; }
+  __device__ __forceinline__ float h_scale(int64_t i) const { return h[i]; }
+};
+
+// four logits of a hidden row from their sums; scales: those of the block's rows, then of its hidden rows
+template <typename P>
+__device__ __forceinline__ f32x4 product_logits(typename P::Acc acc, const float* w_scale, float h_scale) {
+  if constexpr (!P::kScaled) return acc;
+  f32x4 r;
+#pragma unroll
+  for (int v = 0; v < 4; ++v) r[v] = i8_logit((int)acc[v], w_scale[v], h_scale);
+  return r;
+}
+
 constexpr int kWidePad = 32;     // bytes between LDS rows: rows r and r+4 share banks, the 16 lanes of a fragment read never meet
 
 // WR x WH wavefronts (4 or 8); a wavefront owns FR x FH fragments of 16 x 16 logits.
@@ -32,8 +65,8 @@ constexpr int kWidePad = 32;     // bytes between LDS rows: rows r and r+4 share
 // hidden rows in its L2.
 // TAIL: any d % 8 == 0 -- the last step's pieces past column d are fetched from column 0 and parked as zeros, and the
 // number of steps may be odd.  Without it d % (D * BK) == 0.
-template <int WR, int WH, int FR, int FH, int BK, int D, bool TAIL>
-__device__ __forceinline__ void wide_block(const uint32_t blk, const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, const int32_t* __restrict__ ids,
+template <typename P, int WR, int WH, int FR, int FH, int BK, int D, bool TAIL>
+__device__ __forceinline__ void wide_block(const P product, const uint32_t blk, const uint16_t* __restrict__ W, const uint16_t* __restrict__ H, const int32_t* __restrict__ ids,
                                            const int32_t* __restrict__ n_dev, int n_fixed, int V, int batch, int M, int d, int64_t ld, int64_t ids_stride,
                                            float* __restrict__ logits, int row_blocks, int hid_blocks, const int32_t* __restrict__ opos, int opos_len,
                                            int seq_rows, int by_die) {
@@ -109,6 +142,19 @@ __device__ __forceinline__ void wide_block(const uint32_t blk, const uint16_t* _
   const char* Wb = reinterpret_cast<const char*>(W);
   const char* Hbase = reinterpret_cast<const char*>(H);
 
+  // the scales of this block's rows and hidden rows, asked for in front of the operands and parked behind the first step's
+  float scale = 0.f, hscale = 0.f;
+  if constexpr (P::kScaled) {
+    static_assert(BM <= NT && BN <= NT, "a thread a row");
+    if (tid < BM) {
+      int64_t row = j0 + tid < n ? j0 + tid : j0;
+      if (ids) row = ids[row];
+      scale = product.w_scale(row < 0 ? 0 : (row >= V ? V - 1 : row));
+    }
+    if (tid < BN) hscale = product.h_scale((int64_t)b * M + (m0 + tid < M ? m0 + tid : M - 1));
+  }
+  float* scales = reinterpret_cast<float*>(smem + 2 * STAGE);
+
   // D register sets: the loads of step s+D are issued before the matrix work of step s starts, so a load has D
   // steps' time to arrive (one step of matrix work is shorter than an HBM round trip) and D-1 sets -- (D-1) x (BM+BN)
   // x BK x 2 bytes -- are in flight per workgroup all the time
@@ -138,13 +184,14 @@ __device__ __forceinline__ void wide_block(const uint32_t blk, const uint16_t* _
     for (int i = 0; i < NB; ++i) *reinterpret_cast<u32x4*>(Bs + (pr + i * RPP) * STR + pc * 16) = gb[set][i];
   };
 
-  f32x4 acc[FR][FH];
+  typename P::Acc acc[FR][FH];
 #pragma unroll
   for (int a = 0; a < FR; ++a)
 #pragma unroll
-    for (int b = 0; b < FH; ++b) acc[a][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int b = 0; b < FH; ++b) acc[a][b] = typename P::Acc{};
 
-  // fragment addresses: lane = row (mod 16) + 16 * k group, 8 consecutive k (16 bytes) per lane
+  // fragment addresses: lane = row (mod 16) + 16 * k group, a piece of 16 bytes per lane
+  typedef typename P::Piece Piece;
   const int frag_off = (lane & 15) * STR + (lane >> 4) * 16;
   // One step: BK/32 sub-steps of FR x FH matrix instructions.  Operand fragments are asked for one fragment ahead
   // of their use (the next row fragment while the current one's FH instructions run, the next sub-step's hidden-row
@@ -156,36 +203,36 @@ __device__ __forceinline__ void wide_block(const uint32_t blk, const uint16_t* _
     if constexpr (WR * WH != 8) {                     // four wavefronts, memory-bound: the plain order, scheduled by the compiler (205 against 217 us)
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) {
-        bf16x8 bq[FH];
+        Piece bq[FH];
 #pragma unroll
-        for (int b = 0; b < FH; ++b) bq[b] = *reinterpret_cast<const bf16x8*>(Bs + b * 16 * STR + kk * 64);
+        for (int b = 0; b < FH; ++b) bq[b] = *reinterpret_cast<const Piece*>(Bs + b * 16 * STR + kk * 64);
 #pragma unroll
         for (int a = 0; a < FR; ++a) {
-          const bf16x8 aq = *reinterpret_cast<const bf16x8*>(As + a * 16 * STR + kk * 64);
+          const Piece aq = *reinterpret_cast<const Piece*>(As + a * 16 * STR + kk * 64);
 #pragma unroll
-          for (int b = 0; b < FH; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(aq, bq[b], acc[a][b], 0, 0, 0);
+          for (int b = 0; b < FH; ++b) acc[a][b] = P::mul(aq, bq[b], acc[a][b]);
         }
       }
       return;
     }
-    bf16x8 bf[2][FH], af[2];
+    Piece bf[2][FH], af[2];
 #pragma unroll
-    for (int b = 0; b < FH; ++b) bf[0][b] = *reinterpret_cast<const bf16x8*>(Bs + b * 16 * STR);
-    af[0] = *reinterpret_cast<const bf16x8*>(As);
+    for (int b = 0; b < FH; ++b) bf[0][b] = *reinterpret_cast<const Piece*>(Bs + b * 16 * STR);
+    af[0] = *reinterpret_cast<const Piece*>(As);
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) {
 #pragma unroll
       for (int a = 0; a < FR; ++a) {
         const int cur = (kk * FR + a) & 1;
         if (a + 1 < FR) {
-          af[cur ^ 1] = *reinterpret_cast<const bf16x8*>(As + (a + 1) * 16 * STR + kk * 64);
+          af[cur ^ 1] = *reinterpret_cast<const Piece*>(As + (a + 1) * 16 * STR + kk * 64);
         } else if (kk + 1 < KK) {
-          af[cur ^ 1] = *reinterpret_cast<const bf16x8*>(As + (kk + 1) * 64);
+          af[cur ^ 1] = *reinterpret_cast<const Piece*>(As + (kk + 1) * 64);
 #pragma unroll
-          for (int b = 0; b < FH; ++b) bf[(kk + 1) & 1][b] = *reinterpret_cast<const bf16x8*>(Bs + b * 16 * STR + (kk + 1) * 64);
+          for (int b = 0; b < FH; ++b) bf[(kk + 1) & 1][b] = *reinterpret_cast<const Piece*>(Bs + b * 16 * STR + (kk + 1) * 64);
         }
 #pragma unroll
-        for (int b = 0; b < FH; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(af[cur], bf[kk & 1][b], acc[a][b], 0, 0, 0);
+        for (int b = 0; b < FH; ++b) acc[a][b] = P::mul(af[cur], bf[kk & 1][b], acc[a][b]);
       }
     }
     // The order above is the order wanted; left alone, the scheduler puts every fragment read right in front of its
@@ -217,6 +264,10 @@ __device__ __forceinline__ void wide_block(const uint32_t blk, const uint16_t* _
   for (int j = 0; j < D; ++j) fetch(j < nk ? j : nk - 1, j);
   __builtin_amdgcn_sched_barrier(0);
   park(0, 0, 0);
+  if constexpr (P::kScaled) {
+    if (tid < BM) scales[tid] = scale;
+    if (tid < BN) scales[BM + tid] = hscale;
+  }
   __syncthreads();
   for (int ks = 0; ks < nk; ks += D) {
 #pragma unroll
@@ -238,6 +289,7 @@ __device__ __forceinline__ void wide_block(const uint32_t blk, const uint16_t* _
     for (int b = 0; b < FH; ++b) {
       const int m = m0 + (wh * FH + b) * 16 + (lane & 15);
       if (m >= M || j >= n) continue;
+      const f32x4 out = product_logits<P>(acc[a][b], scales + (wr * FR + a) * 16 + 4 * (lane >> 4), P::kScaled ? scales[BM + (wh * FH + b) * 16 + (lane & 15)] : 1.f);
       float* dst = logits + (int64_t)m * ld + j;
       if (opos) {                                       // rows kept in an order of their own: list row j's logits go to column opos[j]
         const int32_t* col = opos + (seq_rows ? (int64_t)(m / seq_rows) * ids_stride : 0);
@@ -246,13 +298,13 @@ __device__ __forceinline__ void wide_block(const uint32_t blk, const uint16_t* _
         float* rowp = logits + (int64_t)m * ld;
 #pragma unroll
         for (int v = 0; v < 4; ++v)
-          if (j + v < n && jo[v] >= 0) rowp[jo[v]] = acc[a][b][v];
+          if (j + v < n && jo[v] >= 0) rowp[jo[v]] = out[v];
       } else if (j + 3 < n) {
-        *reinterpret_cast<f32x4_u*>(dst) = acc[a][b];
+        *reinterpret_cast<f32x4_u*>(dst) = out;
       } else {
 #pragma unroll
         for (int v = 0; v < 4; ++v)
-          if (j + v < n) dst[v] = acc[a][b][v];
+          if (j + v < n) dst[v] = out[v];
       }
     }
   }
@@ -264,7 +316,7 @@ __global__ __launch_bounds__(64 * WR * WH) void head_wide_kernel(const uint16_t*
                                                         int V, int batch, int M, int d, int64_t ld, int64_t ids_stride,
                                                         float* __restrict__ logits, int row_blocks, int hid_blocks,
                                                         const int32_t* __restrict__ opos, int opos_len, int seq_rows, int by_die) {
-  wide_block<WR, WH, FR, FH, BK, D, TAIL>(blockIdx.x, W, H, ids, n_dev, n_fixed, V, batch, M, d, ld, ids_stride, logits, row_blocks, hid_blocks, opos, opos_len, seq_rows, by_die);
+  wide_block<ProductBf16, WR, WH, FR, FH, BK, D, TAIL>({}, blockIdx.x, W, H, ids, n_dev, n_fixed, V, batch, M, d, ld, ids_stride, logits, row_blocks, hid_blocks, opos, opos_len, seq_rows, by_die);
 }
 
 // The list that several sequences share.  Often it is empty -- the device says whether it is used at all --, so its launch is no more workgroups than the chip holds, each of
@@ -278,7 +330,7 @@ __global__ __launch_bounds__(64 * WR * WH) void head_wide_shared_kernel(const ui
   const int n = n_dev[0], used = (n + WR * FR * 16 - 1) / (WR * FR * 16);
   const uint32_t blocks = (uint32_t)((used < row_blocks ? used : row_blocks) + 7) / 8 * 8 * hid_blocks;
   for (uint32_t blk = blockIdx.x; blk < blocks; blk += gridDim.x)
-    wide_block<WR, WH, FR, FH, BK, D, TAIL>(blk, W, H, ids, nullptr, n, V, 1, M, d, ld, opos_stride, logits, row_blocks, hid_blocks, opos, opos_len, seq_rows, 0);
+    wide_block<ProductBf16, WR, WH, FR, FH, BK, D, TAIL>({}, blk, W, H, ids, nullptr, n, V, 1, M, d, ld, opos_stride, logits, row_blocks, hid_blocks, opos, opos_len, seq_rows, 0);
 }
 
 template <int WR, int WH, int FR, int FH, int BK, int D>
@@ -350,7 +402,8 @@ constexpr int kGemmStage = 4 * 128 * 128;        // bytes of one stage: A0, A1, 
 // 1024 hidden rows on the 128k x 4096 matrix: 896 us = 1.20 PFLOP/s (head_wide_kernel's 256 x 256 shape: 1036); the loop takes
 // 1.16 times its matrix cycles, at the 1.7 GHz this load runs at.  512 hidden rows 532 -> 490 us, 130: 309 -> 275.  The
 // sums are taken in the same order: results are bit-equal.
-__global__ __launch_bounds__(512, 2) void head_gemm_kernel(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H,
+template <typename P>
+__device__ __forceinline__ void gemm_block(const P product, const uint16_t* __restrict__ W, const uint16_t* __restrict__ H,
                                                            const int32_t* __restrict__ ids, const int32_t* __restrict__ n_dev, int n_fixed,
                                                            int V, int M, int d, int64_t ld, float* __restrict__ logits, int row_blocks,
                                                            int hid_blocks, const int32_t* __restrict__ opos, int opos_len) {
@@ -411,37 +464,49 @@ __global__ __launch_bounds__(512, 2) void head_gemm_kernel(const uint16_t* __res
     lds_fetch16(l + 1024, base, boff[h][1]);
   };
 
-  f32x4 acc[8][4];
+  float* scales = reinterpret_cast<float*>(smem + 2 * kGemmStage);
+  if constexpr (P::kScaled) {                              // waited for by the first counted wait, which leaves the operands' fetches in flight
+    if (tid < 256) {
+      int64_t row = j0 + tid < n ? j0 + tid : j0;
+      if (ids) row = ids[row];
+      scales[tid] = product.w_scale(row < 0 ? 0 : (row >= V ? V - 1 : row));
+    } else {
+      scales[tid] = product.h_scale(m0 + tid - 256 < M ? m0 + tid - 256 : M - 1);
+    }
+  }
+
+  typedef typename P::Piece Piece;
+  typename P::Acc acc[8][4];
 #pragma unroll
   for (int a = 0; a < 8; ++a)
 #pragma unroll
-    for (int b = 0; b < 4; ++b) acc[a][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int b = 0; b < 4; ++b) acc[a][b] = typename P::Acc{};
 
   // fragment addresses inside a half: row r (lane & 15 within the fragment), piece (lane >> 4) + 4 * kk, swizzled by r & 7
   const int fr = lane & 15, s7 = lane & 7;
   const uint32_t f0 = fr * 128 + (((lane >> 4)) ^ s7) * 16, f1 = fr * 128 + (((lane >> 4) + 4) ^ s7) * 16;
-  bf16x8 af[4][2], b0[2][2], b1[2][2], b2[2][2];
+  Piece af[4][2], b0[2][2], b1[2][2], b2[2][2];
   auto read_a = [&](int st, int h) {
     const char* p = smem + (st & 1) * kGemmStage + h * 16384 + wr * 8192;
 #pragma unroll
     for (int a = 0; a < 4; ++a) {
-      af[a][0] = *reinterpret_cast<const bf16x8*>(p + a * 2048 + f0);
-      af[a][1] = *reinterpret_cast<const bf16x8*>(p + a * 2048 + f1);
+      af[a][0] = *reinterpret_cast<const Piece*>(p + a * 2048 + f0);
+      af[a][1] = *reinterpret_cast<const Piece*>(p + a * 2048 + f1);
     }
   };
-  auto read_b = [&](int st, int h, bf16x8(&bq)[2][2]) {
+  auto read_b = [&](int st, int h, Piece(&bq)[2][2]) {
     const char* p = smem + (st & 1) * kGemmStage + 32768 + h * 16384 + wh * 4096;
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      bq[b][0] = *reinterpret_cast<const bf16x8*>(p + b * 2048 + f0);
-      bq[b][1] = *reinterpret_cast<const bf16x8*>(p + b * 2048 + f1);
+      bq[b][0] = *reinterpret_cast<const Piece*>(p + b * 2048 + f0);
+      bq[b][1] = *reinterpret_cast<const Piece*>(p + b * 2048 + f1);
     }
   };
 #define NS_COMPUTE(A0, B0, bq)                                                                                                          \
   do {                                                                                                                                  \
     __builtin_amdgcn_s_setprio(1);                                                                                                      \
     _Pragma("unroll") for (int kk = 0; kk < 2; ++kk) _Pragma("unroll") for (int a = 0; a < 4; ++a) _Pragma("unroll") for (int b = 0; b < 2; ++b) \
-        acc[A0 + a][B0 + b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(af[a][kk], bq[b][kk], acc[A0 + a][B0 + b], 0, 0, 0);             \
+        acc[A0 + a][B0 + b] = P::mul(af[a][kk], bq[b][kk], acc[A0 + a][B0 + b]);             \
     __builtin_amdgcn_s_setprio(0);                                                                                                      \
   } while (0)
 
@@ -457,7 +522,7 @@ __global__ __launch_bounds__(512, 2) void head_gemm_kernel(const uint16_t* __res
   NS_BARRIER();
   read_b(0, 0, b0);
   if (wr == 1) NS_BARRIER();                               // the second four wavefronts run one cluster behind the first
-  auto step = [&](int st, bf16x8(&bc)[2][2], bf16x8(&bn)[2][2]) {
+  auto step = [&](int st, Piece(&bc)[2][2], Piece(&bn)[2][2]) {
     read_a(st, 0);
     fetch_a(st + 1, 1);
     NS_WAIT_VM(10);
@@ -498,22 +563,36 @@ __global__ __launch_bounds__(512, 2) void head_gemm_kernel(const uint16_t* __res
     for (int b = 0; b < 4; ++b) {
       const int m = m0 + wh * 64 + b * 16 + (lane & 15);
       if (m >= M || j >= n) continue;
+      const f32x4 out = product_logits<P>(acc[a][b], scales + wr * 128 + a * 16 + 4 * (lane >> 4), P::kScaled ? scales[256 + wh * 64 + b * 16 + (lane & 15)] : 1.f);
       float* rowp = logits + (int64_t)m * ld;
       if (opos) {
         const int4 jo4 = j + 3 < opos_len ? *reinterpret_cast<const int4*>(opos + j) : make_int4(-1, -1, -1, -1);
         const int jo[4] = {jo4.x, jo4.y, jo4.z, jo4.w};
 #pragma unroll
         for (int v = 0; v < 4; ++v)
-          if (j + v < n && jo[v] >= 0) rowp[jo[v]] = acc[a][b][v];
+          if (j + v < n && jo[v] >= 0) rowp[jo[v]] = out[v];
       } else if (j + 3 < n) {
-        *reinterpret_cast<f32x4_u*>(rowp + j) = acc[a][b];
+        *reinterpret_cast<f32x4_u*>(rowp + j) = out;
       } else {
 #pragma unroll
         for (int v = 0; v < 4; ++v)
-          if (j + v < n) rowp[j + v] = acc[a][b][v];
+          if (j + v < n) rowp[j + v] = out[v];
       }
     }
   }
+}
+
+__global__ __launch_bounds__(512, 2) void head_gemm_kernel(const uint16_t* __restrict__ W, const uint16_t* __restrict__ H,
+                                                           const int32_t* __restrict__ ids, const int32_t* __restrict__ n_dev, int n_fixed,
+                                                           int V, int M, int d, int64_t ld, float* __restrict__ logits, int row_blocks,
+                                                           int hid_blocks, const int32_t* __restrict__ opos, int opos_len) {
+  gemm_block<ProductBf16>({}, W, H, ids, n_dev, n_fixed, V, M, d, ld, logits, row_blocks, hid_blocks, opos, opos_len);
+}
+
+__global__ __launch_bounds__(512, 2) void head_gemm_i8_kernel(const ProductI8 product, const uint16_t* __restrict__ W, const uint16_t* __restrict__ H,
+                                                              const int32_t* __restrict__ ids, const int32_t* __restrict__ n_dev, int n_fixed,
+                                                              int V, int M, int d, int64_t ld, float* __restrict__ logits, int row_blocks, int hid_blocks) {
+  gemm_block(product, W, H, ids, n_dev, n_fixed, V, M, d, ld, logits, row_blocks, hid_blocks, nullptr, 0);
 }
 
 static hipError_t run_gemm(const uint16_t* W, const uint16_t* H, const int32_t* ids, const int32_t* n_dev, int32_t n_fixed, int32_t cap_rows,
@@ -524,6 +603,90 @@ static hipError_t run_gemm(const uint16_t* W, const uint16_t* H, const int32_t* 
   head_gemm_kernel<<<dim3((unsigned)grid), 512, 2 * kGemmStage, s>>>(W, H, ids, n_dev, n_fixed, V, M, d, ld, logits, row_blocks, hid_blocks, opos,
                                                                      cap_rows / 4 * 4);
   return hipGetLastError();
+}
+
+// The 8-bit head: rows in pairs of columns (d2 = d / 2), the hidden rows quantized, the same block shapes.
+template <int WR, int WH, int FR, int FH, int BK, int D, bool TAIL>
+__global__ __launch_bounds__(64 * WR * WH) void head_wide_i8_kernel(const ProductI8 product, const uint16_t* __restrict__ W, const uint16_t* __restrict__ H,
+                                                           const int32_t* __restrict__ ids, const int32_t* __restrict__ n_dev, int n_fixed, int V, int batch,
+                                                           int M, int d2, int64_t ld, int64_t ids_stride, float* __restrict__ logits, int row_blocks,
+                                                           int hid_blocks, int by_die) {
+  wide_block<ProductI8, WR, WH, FR, FH, BK, D, TAIL>(product, blockIdx.x, W, H, ids, n_dev, n_fixed, V, batch, M, d2, ld, ids_stride, logits, row_blocks, hid_blocks,
+                                                     nullptr, 0, 0, by_die);
+}
+
+constexpr int kI8Lds(int BM, int BN, int BK) { return 2 * (BM + BN) * (BK * 2 + kWidePad) + (BM + BN) * 4; }
+
+template <int WR, int WH, int FR, int FH, int BK, int D>
+static hipError_t run_wide_i8(ProductI8 product, const uint16_t* W, const uint16_t* H, const int32_t* ids, const int32_t* n_dev, int32_t cap_rows, int32_t V, int32_t batch,
+                              int32_t M, int32_t d2, int64_t ld, float* logits, int by_die, hipStream_t s) {
+  constexpr int BM = WR * FR * 16, BN = WH * FH * 16, LDS = kI8Lds(BM, BN, BK);
+  const int row_blocks = (cap_rows + BM - 1) / BM, hid_blocks = (M + BN - 1) / BN;
+  const int64_t grid = batch == 1 || by_die ? (int64_t)((row_blocks + 7) / 8) * hid_blocks * batch * 8 : (int64_t)row_blocks * hid_blocks * batch;
+  if (grid > 0x7fffffff || !wide_reaches(V, M, d2)) return hipErrorInvalidValue;
+#define NS_WIDE_I8(TAIL)                                                                                                                     \
+  head_wide_i8_kernel<WR, WH, FR, FH, BK, D, TAIL><<<dim3((unsigned)grid), 64 * WR * WH, LDS, s>>>(product, W, H, ids, n_dev, cap_rows, V, batch, M, d2, ld, cap_rows, logits, \
+                                                                                                   row_blocks, hid_blocks, by_die)
+  if (d2 % (D * BK) == 0) NS_WIDE_I8(false);
+  else NS_WIDE_I8(true);
+#undef NS_WIDE_I8
+  return hipGetLastError();
+}
+
+hipError_t launch_head_wide_i8(const int8_t* W, const float* W_scale, const int8_t* H, const float* H_scale, const int32_t* ids, const int32_t* n_dev, int32_t cap_rows,
+                               int32_t V, int32_t batch, int32_t M, int32_t d, int64_t ld, float* logits, hipStream_t s) {
+  const uint16_t* Wp = reinterpret_cast<const uint16_t*>(W);
+  const uint16_t* Hp = reinterpret_cast<const uint16_t*>(H);
+  const ProductI8 product{W_scale, H_scale};
+  const bool dense = n_dev == nullptr;
+  const WideShape shape = i8_shape(M, d, batch, cap_rows, dense);
+  if (shape == kWideGemm) {
+    const int row_blocks = (cap_rows + 255) / 256, hid_blocks = (M + 255) / 256;
+    const int64_t grid = (int64_t)((row_blocks + 7) / 8) * hid_blocks * 8;
+    if (grid > 0x7fffffff) return hipErrorInvalidValue;
+    head_gemm_i8_kernel<<<dim3((unsigned)grid), 512, 2 * kGemmStage + 2048, s>>>(product, Wp, Hp, ids, n_dev, cap_rows, V, M, d / 2, ld, logits, row_blocks, hid_blocks);
+    return hipGetLastError();
+  }
+  const int by_die = (int)wide_by_die(M, batch, cap_rows, dense);
+#define NS_SHAPE(S) \
+  case S: return run_wide_i8<kWideBlocks[S].WR, kWideBlocks[S].WH, kWideBlocks[S].FR, kWideBlocks[S].FH, kWideBlocks[S].BK, kWideBlocks[S].D>(product, Wp, Hp, ids, n_dev, cap_rows, V, batch, M, d / 2, ld, logits, by_die, s)
+  switch (shape) {
+    NS_SHAPE(kWide32x16);
+    NS_SHAPE(kWide64x16);
+    NS_SHAPE(kWide32x32);
+    NS_SHAPE(kWide64x32);
+    NS_SHAPE(kWide32x64);
+    NS_SHAPE(kWide64x64);
+    NS_SHAPE(kWide128x64);
+    NS_SHAPE(kWide256x128);
+    default: return hipErrorInvalidValue;
+  }
+#undef NS_SHAPE
+}
+
+template <WideShape SHAPE>
+static hipError_t configure_i8() {
+  constexpr WideBlock b = kWideBlocks[SHAPE];
+  const void* fns[] = {reinterpret_cast<const void*>(head_wide_i8_kernel<b.WR, b.WH, b.FR, b.FH, b.BK, b.D, false>),
+                       reinterpret_cast<const void*>(head_wide_i8_kernel<b.WR, b.WH, b.FR, b.FH, b.BK, b.D, true>)};
+  for (const void* f : fns) {
+    hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+static hipError_t configure_wide_i8() {
+  hipError_t e = configure_i8<kWide32x16>();
+  if (e == hipSuccess) e = configure_i8<kWide64x16>();
+  if (e == hipSuccess) e = configure_i8<kWide32x32>();
+  if (e == hipSuccess) e = configure_i8<kWide64x32>();
+  if (e == hipSuccess) e = configure_i8<kWide32x64>();
+  if (e == hipSuccess) e = configure_i8<kWide64x64>();
+  if (e == hipSuccess) e = configure_i8<kWide128x64>();
+  if (e == hipSuccess) e = configure_i8<kWide256x128>();
+  if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(head_gemm_i8_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+  return e;
 }
 
 template <WideShape SHAPE>
@@ -549,7 +712,8 @@ static hipError_t configure_wide() {
 }
 
 hipError_t wide_configure_device() {
-  hipError_t e = configure_wide<kWide32x16>();
+  hipError_t e = configure_wide_i8();
+  if (e == hipSuccess) e = configure_wide<kWide32x16>();
   if (e == hipSuccess) e = configure_wide<kWide64x16>();
   if (e == hipSuccess) e = configure_wide<kWide32x32>();
   if (e == hipSuccess) e = configure_wide<kWide64x32>();
