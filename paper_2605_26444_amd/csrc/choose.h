@@ -127,7 +127,51 @@ inline WideShape wide_shape(int32_t M, int32_t d, int32_t batch, int32_t cap_row
   return d % 64 == 0 && aligned ? kWideGemm : kWide256x256;
 }
 
-// The 8-bit head's: as many bytes a step hold twice the columns.  256 x 256 blocks with the scales do not fit LDS, so d that is no multiple of 128 takes 256 x 128.
+// ---- the 8-bit head for up to 16 hidden rows (few8.hip) --------------------------------------------------------------
+
+struct FewPlan {
+  int32_t KS, slices, log_groups, waves, log_parts, seg, lds;   // loads per step and slice, slices of a row, groups of rows (log2), wavefronts, pieces of a list per die (log2), steps of a segment, bytes
+};
+
+// What it takes: at most eight slices.
+inline bool few_supported(int32_t M, int32_t d) { return M <= 16 && d <= (M <= 8 ? 16384 : 8192); }
+
+// Whether it rounds the hidden rows itself, in every workgroup, or takes them from a launch of their own (3 us): 3000 rows of 4096, M = 8 6.8 us against 8.9, M = 1 5.4 / 8.0;
+// M = 16 10.6 / 9.8; 8192 columns, whose second half a workgroup reads twice, M = 4 12.3 / 10.7, M = 8 13.9 / 11.2.
+inline bool few_rounds(int32_t M, int32_t d) { return d <= 4096 && (int64_t)M * d <= 32768; }
+
+// Shapes, us on lists of n live rows or dense (n = V = 128256), with 8 | 4 wavefronts:
+//   * few bytes (room for less than 48 MB of rows): a row cut into as many slices as there are wavefronts, so that a workgroup reads its hidden rows from LDS once
+//     and not once a group -- 3000 x 4096, M = 8: KS = 2 6.8, 4 8.0, 8 8.0; 8000 x 4096 M = 8 9.7 / 10.6 / 10.6, M = 16 12.7 / 13.7; 1000 x 1024 M = 8 5.2 / 6.3;
+//   * many: longer steps, fewer wavefronts to a workgroup -- 32000 x 4096 M = 8: KS = 2 31.6, 4 33.3 | 32.4, 8 33.3 | 31.8; dense x 4096 M = 8 93.6, 104 | 93, 102 | 91.3, M = 16 98.9,
+//     107 | 97.7; 64 sequences of 2300 x 4096 M = 8 67.6, 66.7 | 62, 66.8 | 60.8; rows up to 2048 bytes dense M = 8 47.3, 45.3 | 47.8, 46.6 | 46.9, 512 bytes 13.7, 14.4 | 16.
+// 256 workgroups (twice as many: the second half waits for the first and rounds the hidden rows again: 8.6 us for 6.8, 97 for 93.6).
+inline FewPlan few_plan(int32_t M, int32_t d, int32_t batch, int32_t cap_rows, bool rounds) {
+  FewPlan f;
+  const bool many = (int64_t)cap_rows * batch * d >= 48000000;
+  const int32_t least = d <= 4096 ? 2 : d <= 8192 ? 4 : 8;
+  f.KS = !many || d <= 512 ? least : d <= 2048 || M > 8 ? 4 : 8;
+  f.slices = (d + 256 * f.KS - 1) / (256 * f.KS);
+  const int32_t most = many && d > 2048 ? 4 : 8;                        // wavefronts
+  f.log_groups = 0;
+  while (f.slices << (f.log_groups + 1) <= most) ++f.log_groups;
+  f.waves = f.slices << f.log_groups;
+  f.log_parts = 0;
+  while (f.log_parts < 5 && 8 * batch << f.log_parts < 256) ++f.log_parts;
+  const int32_t mh = M <= 4 ? 4 : M <= 8 ? 8 : 16, rows = 4 << f.log_groups;
+  // a segment: the longest piece, two scales a thread, what LDS holds; a multiple of the steps in flight
+  const int64_t blocks = ((int64_t)cap_rows + rows - 1) / rows, longest = (blocks + (8ll << f.log_parts) - 1) >> (3 + f.log_parts);
+  const int64_t room = (72 * 1024 / 4 - f.slices * mh * 4) / (f.slices * mh + 1) / rows;
+  int64_t seg = (longest + 3) / 4 * 4;
+  if (seg > 128 * f.waves / rows) seg = 128 * f.waves / rows;
+  if (seg > room) seg = room;
+  f.seg = (int32_t)(seg / 4 * 4);
+  const int64_t sums = (int64_t)f.slices * mh * (rows * f.seg + 4) * 4, hidden = rounds ? (int64_t)M * (d + 16) : 0;
+  f.lds = (int32_t)(64 + 4 * rows * f.seg + (sums > hidden ? sums : hidden));
+  return f;
+}
+
+// The 8-bit head's block shapes beyond: as many bytes a step hold twice the columns.  256 x 256 blocks with the scales do not fit LDS, so d that is no multiple of 128 takes 256 x 128.
 inline WideShape i8_shape(int32_t M, int32_t d, int32_t batch, int32_t cap_rows, bool dense) {
   const WideShape s = wide_shape(M, d / 2, batch, cap_rows, dense, d % 128 == 0);
   return s == kWide256x256 ? kWide256x128 : s;

@@ -49,50 +49,65 @@ __device__ __forceinline__ void lds_fetch16(uint32_t lds, const void* base, uint
 }
 #pragma clang diagnostic pop
 
-// A row in 8 bits (quant.hip): a = max |x|, scale = a / 127, q = 127 x / a to the nearest integer, ties to even.
-// Computed on x and a times a power of two that leaves a in [0.5, 1), in two factors, so that nothing overflows and a is no denormal; what
-// the factors lose of a tiny x rounds to q = 0 either way.  127 x of a bf16 x is exact in fp32 (15 bits) and so is the decision: the
-// quotient of a 15-bit by an 8-bit number is a tie or at least 2^-9 away from one, and the quotient here -- by the reciprocal, with one
-// correction -- is exact if it is a tie and 2^-16 off at most otherwise.  So q is what exact arithmetic gives.
+template <bool B>
+struct Flag {
+  static constexpr bool value = B;
+};
+
+// A row in 8 bits (quant.hip): a = max |x|, scale = a / 127, q = 127 x / a to the nearest integer, ties to even -- of the exact quotient.
+// One multiplication with 127 / a rounded up, rounded to an integer once, gives that for every bf16 x:
+//   * a tie is 254 x / a = an odd integer.  a and x are 8-bit numbers times powers of two, so 127 divides that integer, and the tie
+//     is |x| = a / 2, q = 63.5, or a is 254 times a power of two;
+//   * in the latter case 127 / a is a power of two and the product exact;
+//   * in the former the product is 63.5 or a little more, and rounds to 64, which is even;
+//   * any other quotient is 2^-9 away from a tie at least (a difference of fractions over 2 a), the product within 127 * 2^-23 of it.
+// Where a is below 2^-64, p = 2^64 keeps 127 / (a p) a number; elsewhere it is 1 and left out.
 struct I8Row {
-  float p, p127, a, r;
-  uint32_t mask;       // 0: a row of zeros, or one with an infinity or a NaN: all q are 0
+  float p, inv;        // inv is 0 for a row of zeros and for one with an infinity or a NaN: x inv is 0 or a NaN, whose low byte is 0
   float scale;
 };
 
-// top: the largest magnitude's bits (of all the row's numbers, signs cleared: an infinity or a NaN is larger than any number)
-__device__ __forceinline__ I8Row i8_row(uint32_t top_bits) {
-  I8Row k;
-  const bool bad = top_bits >= 0x7f800000u;
-  const float top = __uint_as_float(top_bits);
-  const int e = bad || top_bits == 0 ? 0 : __builtin_amdgcn_frexp_expf(top);
-  const int e1 = e >> 1, e2 = e - e1;
-  k.p = __uint_as_float((uint32_t)(127 - e1) << 23);
-  k.p127 = 127.f * __uint_as_float((uint32_t)(127 - e2) << 23);
-  k.mask = bad || top_bits == 0 ? 0u : 0xffffffffu;
-  k.a = k.mask ? top * k.p * __uint_as_float((uint32_t)(127 - e2) << 23) : 1.f;
-  k.r = 1.f / k.a;
-  k.scale = bad ? __builtin_nanf("") : top / 127.f;
-  return k;
+// top: the largest magnitude of the row as the upper half of an fp32, sign cleared: an infinity or a NaN is larger than any number
+__device__ __forceinline__ I8Row i8_row(uint32_t top) {
+  const float a = __uint_as_float(top << 16);
+  const bool bad = top >= 0x7f80u, none = bad || top == 0;
+  const float p = a < 0x1p-64f && !none ? 0x1p64f : 1.f, ap = none ? 1.f : a * p;
+  const float r = 127.f / ap;
+  const float up = __uint_as_float(__float_as_uint(r) + (fmaf(r, ap, -127.f) < 0.f ? 1u : 0u));
+  return I8Row{p, none ? 0.f : up, bad ? __builtin_nanf("") : a / 127.f};
 }
 
 // q of one number in the low byte: adding 1.5 * 2^23 rounds to an integer
+template <bool TINY>
 __device__ __forceinline__ uint32_t i8_round(const I8Row& k, uint32_t x_bits) {
-  const float n = __uint_as_float(x_bits & k.mask) * k.p * k.p127, q = n * k.r;
-  return __float_as_uint(fmaf(fmaf(-q, k.a, n), k.r, q) + 12582912.f);
+  const float x = __uint_as_float(x_bits);
+  return __float_as_uint(fmaf(TINY ? x * k.p : x, k.inv, 12582912.f));
 }
 
 // four numbers of two bf16 pairs
+template <bool TINY>
 __device__ __forceinline__ uint32_t i8_round4(const I8Row& k, uint32_t x01, uint32_t x23) {
-  const uint32_t a = i8_round(k, x01 << 16), b = i8_round(k, x01 & 0xffff0000u), c = i8_round(k, x23 << 16), d = i8_round(k, x23 & 0xffff0000u);
+  const uint32_t a = i8_round<TINY>(k, x01 << 16), b = i8_round<TINY>(k, x01 & 0xffff0000u), c = i8_round<TINY>(k, x23 << 16), d = i8_round<TINY>(k, x23 & 0xffff0000u);
   return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400u), __builtin_amdgcn_perm(b, a, 0x0c0c0400u), 0x05040100u);
 }
 
-// largest magnitude of eight bf16, as the bits of an fp32 with the sign cleared
-__device__ __forceinline__ uint32_t bf16_top(uint32_t top, uint32_t x) {
-  const uint32_t lo = (x << 16) & 0x7fff0000u, hi = x & 0x7fff0000u;
-  const uint32_t m = lo > hi ? lo : hi;
-  return m > top ? m : top;
+// larger magnitudes of two bf16 pairs, position by position
+__device__ __forceinline__ uint32_t bf16_tops(uint32_t top, uint32_t x) {
+  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, top), __builtin_bit_cast(u16x2, x & 0x7fff7fffu)));
+}
+
+// the largest of all positions of all lanes
+__device__ __forceinline__ uint32_t wave_top(uint32_t tops) {
+  uint32_t x = tops >> 16 > (tops & 0xffffu) ? tops >> 16 : tops & 0xffffu;
+  auto step = [&](uint32_t y) { x = y > x ? y : x; };
+  step(__builtin_amdgcn_update_dpp(0, x, 0xB1, 0xf, 0xf, false));      // as row_sum: every lane of a row of 16 ends with the row's
+  step(__builtin_amdgcn_update_dpp(0, x, 0x4E, 0xf, 0xf, false));
+  step(__builtin_amdgcn_update_dpp(0, x, 0x141, 0xf, 0xf, false));
+  step(__builtin_amdgcn_update_dpp(0, x, 0x140, 0xf, 0xf, false));
+  const uint32_t a = __builtin_amdgcn_readlane(x, 0), b = __builtin_amdgcn_readlane(x, 16), c = __builtin_amdgcn_readlane(x, 32), d = __builtin_amdgcn_readlane(x, 48);
+  const uint32_t ab = a > b ? a : b, cd = c > d ? c : d;
+  return ab > cd ? ab : cd;
 }
 
 // A logit of the 8-bit heads: the integer sum rounded to fp32, then the two scales' product.  All kernels round in these places.
@@ -265,6 +280,11 @@ int64_t head_i8_workspace_bytes(int32_t rows, int32_t d);
 hipError_t launch_quantize_rows(const void* X, int64_t rows, int32_t d, int8_t* q, float* scale, hipStream_t s);
 hipError_t launch_head_i8(const int8_t* W, const float* W_scale, const void* H, const int32_t* ids, const int32_t* n_dev, int32_t cap_rows, int32_t V, int32_t batch,
                           int32_t M, int32_t d, int64_t ld, float* logits, char* ws, hipStream_t s);
+
+// few8.hip: up to 16 hidden rows; H in bf16, or null and the rows rounded before
+hipError_t few_configure_device();
+hipError_t launch_head_few_i8(const int8_t* W, const float* W_scale, const void* H, const int8_t* Hq, const float* H_scale, const int32_t* ids, const int32_t* n_dev,
+                              int32_t cap_rows, int32_t V, int32_t batch, int32_t M, int32_t d, int64_t ld, float* logits, hipStream_t s);
 
 // loss.hip
 int64_t loss_workspace_bytes(int32_t rows, int32_t V);

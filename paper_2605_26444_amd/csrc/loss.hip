@@ -20,9 +20,10 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8_any __attribute__((ext_vector_type(8), aligned(2)));
 
 constexpr int kRowThreads = 256;
-constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLog2e = 0x1.715476p+0f, kLog2eRest = 0x1.4ae0c0p-26f, kLn2 = 0.6931471805599453f;   // log2 e in two parts
 
-__device__ __forceinline__ float exp_neg(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }   // x <= 0: the relative error is 2^-24 |x| at most beside the instruction's
+// x <= 0: off by 2^-24 (2 |x| + 2) of the result at most
+__device__ __forceinline__ float exp_neg(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
 template <typename T>
 struct Vec;
@@ -82,16 +83,28 @@ __device__ __forceinline__ Stat join(Stat a, Stat b) {
   return Stat{m, a.s * exp_neg(a.m - mm) + b.s * exp_neg(b.m - mm)};
 }
 
+// N more numbers.  exp(x - m) = 2^(L x - L m) with L = log2 e in two parts: rounded to one fp32, L would lower every exponent by 1.3e-8 of
+// itself, an error that does not average out over a row (1e-7 of the sum, seen in the margin of two answers, where most of
+// the log-probabilities cancels).  L x - c in two multiply-adds, as many instructions as x - m and a product; c = fl(L m), and what c is off
+// by multiplies the sum.
 template <int N>
 __device__ __forceinline__ void take(Stat& t, const float (&x)[N]) {
   float top = x[0];
 #pragma unroll
   for (int i = 1; i < N; ++i) top = fmaxf(top, x[i]);
-  const float m = fmaxf(t.m, top), mm = finite_or_zero(m);
+  const float m = fmaxf(t.m, top);
   float s = 0.f;
+  if (fabsf(m) < 1e37f) {
+    const float c = m * kLog2e, off = fmaf(m, kLog2eRest, fmaf(m, kLog2e, -c));
 #pragma unroll
-  for (int i = 0; i < N; ++i) s += exp_neg(x[i] - mm);
-  t.s = t.s * exp_neg(t.m - mm) + s;
+    for (int i = 0; i < N; ++i) s += __builtin_amdgcn_exp2f(fmaf(x[i], kLog2eRest, fmaf(x[i], kLog2e, -c)));
+    s = fmaf(s, -off * kLn2, s);
+  } else {                                                 // nothing but -inf so far, or L m does not fit
+    const float mm = finite_or_zero(m);
+#pragma unroll
+    for (int i = 0; i < N; ++i) s += exp_neg(x[i] - mm);
+  }
+  t.s = t.s * exp_neg(t.m - finite_or_zero(m)) + s;
   t.m = m;
 }
 

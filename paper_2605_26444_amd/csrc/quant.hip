@@ -6,35 +6,66 @@ namespace nanospec {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-// A wavefront a row; the row is read twice, the second time from the caches.
-__global__ __launch_bounds__(256) void quantize_rows_kernel(const uint16_t* __restrict__ X, int64_t rows, int d, int8_t* __restrict__ q, float* __restrict__ scale) {
-  const int lane = threadIdx.x & 63;
-  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row >= rows) return;
+// WPR wavefronts a row, which holds what they can of it -- 32 numbers a lane -- in registers and reads the rest again, from the caches.
+template <int WPR>
+__global__ __launch_bounds__(WPR < 4 ? 256 : 64 * WPR) void quantize_rows_kernel(const uint16_t* __restrict__ X, int64_t rows, int d, int8_t* __restrict__ q,
+                                                                               float* __restrict__ scale) {
+  constexpr int P = 4, RPB = WPR < 4 ? 4 / WPR : 1, STEP = 512 * WPR;
+  const int tid = threadIdx.x, at = WPR < 4 ? tid % (64 * WPR) : tid;
+  const int64_t row = (int64_t)blockIdx.x * RPB + (RPB > 1 ? tid / (64 * WPR) : 0);
+  if (row >= rows) return;                                 // whole rows of a workgroup only where wavefronts do not meet
   const uint16_t* x = X + row * d;
-  uint32_t top = 0;
-  for (int c = lane * 8; c < d; c += 512) {
-    const u32x4 v = *reinterpret_cast<const u32x4*>(x + c);
+  u32x4 v[P];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) top = bf16_top(top, v[i]);
+  for (int i = 0; i < P; ++i) {
+    const int c = at * 8 + i * STEP;
+    v[i] = *reinterpret_cast<const u32x4*>(x + (c < d ? c : 0));          // past the end a copy of the row's first
   }
+  uint32_t top = 0;
 #pragma unroll
-  for (int o = 32; o; o >>= 1) {
-    const uint32_t t = __shfl_xor(top, o);
-    top = t > top ? t : top;
+  for (int i = 0; i < P; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) top = bf16_tops(top, v[i][e]);
+  for (int c = at * 8 + P * STEP; c < d; c += STEP) {
+    const u32x4 y = *reinterpret_cast<const u32x4*>(x + c);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) top = bf16_tops(top, y[e]);
+  }
+  top = wave_top(top);
+  if (WPR > 1) {
+    __shared__ uint32_t tops[WPR];
+    if ((tid & 63) == 0) tops[tid >> 6] = top;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < WPR; ++i) top = tops[i] > top ? tops[i] : top;
   }
   const I8Row k = i8_row(top);
-  for (int c = lane * 8; c < d; c += 512) {
-    const u32x4 v = *reinterpret_cast<const u32x4*>(x + c);
-    *reinterpret_cast<u32x2*>(q + row * d + c) = u32x2{i8_round4(k, v[0], v[1]), i8_round4(k, v[2], v[3])};
-  }
-  if (lane == 0) scale[row] = k.scale;
+  auto put = [&](auto tiny) {
+    auto one = [&](int c, const u32x4 y) {
+      constexpr bool T = decltype(tiny)::value;
+      *reinterpret_cast<u32x2*>(q + row * d + c) = u32x2{i8_round4<T>(k, y[0], y[1]), i8_round4<T>(k, y[2], y[3])};
+    };
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int c = at * 8 + i * STEP;
+      if (c < d) one(c, v[i]);
+    }
+    for (int c = at * 8 + P * STEP; c < d; c += STEP) one(c, *reinterpret_cast<const u32x4*>(x + c));
+  };
+  if (k.p == 1.f) put(Flag<false>());
+  else put(Flag<true>());
+  if (at == 0) scale[row] = k.scale;
 }
 
+// Many rows: as few wavefronts a row as hold it.  Few: as many as there are numbers for, since a row's time is what a wavefront's chain of loads and rounding takes.
 hipError_t launch_quantize_rows(const void* X, int64_t rows, int32_t d, int8_t* q, float* scale, hipStream_t s) {
-  const int64_t grid = (rows + 3) / 4;
+  const uint16_t* x = static_cast<const uint16_t*>(X);
+  const int wpr = rows >= 2048 ? (d <= 2048 ? 1 : d <= 8192 ? 4 : 16) : (d <= 512 ? 1 : d <= 2048 ? 4 : 16);
+  const int64_t grid = wpr == 1 ? (rows + 3) / 4 : rows;
   if (grid > 0x7fffffff) return hipErrorInvalidValue;
-  quantize_rows_kernel<<<dim3((unsigned)grid), 256, 0, s>>>(static_cast<const uint16_t*>(X), rows, d, q, scale);
+  if (wpr == 1) quantize_rows_kernel<1><<<dim3((unsigned)grid), 256, 0, s>>>(x, rows, d, q, scale);
+  else if (wpr == 4) quantize_rows_kernel<4><<<dim3((unsigned)grid), 256, 0, s>>>(x, rows, d, q, scale);
+  else quantize_rows_kernel<16><<<dim3((unsigned)grid), 1024, 0, s>>>(x, rows, d, q, scale);
   return hipGetLastError();
 }
 
@@ -45,9 +76,12 @@ int64_t head_i8_workspace_bytes(int32_t rows, int32_t d) { return rows_bytes(row
 
 hipError_t launch_head_i8(const int8_t* W, const float* W_scale, const void* H, const int32_t* ids, const int32_t* n_dev, int32_t cap_rows, int32_t V, int32_t batch,
                           int32_t M, int32_t d, int64_t ld, float* logits, char* ws, hipStream_t s) {
+  const bool few = few_supported(M, d);
+  if (few && few_rounds(M, d)) return launch_head_few_i8(W, W_scale, H, nullptr, nullptr, ids, n_dev, cap_rows, V, batch, M, d, ld, logits, s);
   int8_t* q = reinterpret_cast<int8_t*>(ws);
   float* scale = reinterpret_cast<float*>(ws + rows_bytes(batch * M, d));
   hipError_t e = launch_quantize_rows(H, (int64_t)batch * M, d, q, scale, s);
+  if (e == hipSuccess && few) return launch_head_few_i8(W, W_scale, nullptr, q, scale, ids, n_dev, cap_rows, V, batch, M, d, ld, logits, s);
   return e == hipSuccess ? launch_head_wide_i8(W, W_scale, q, scale, ids, n_dev, cap_rows, V, batch, M, d, ld, logits, s) : e;
 }
 

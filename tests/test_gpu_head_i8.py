@@ -70,6 +70,27 @@ def test_rows_are_rounded_as_exact_arithmetic_rounds_them(rows, d):
     assert (q[n] == 99).all() and scale[n] == -7.0
 
 
+@pytest.mark.parametrize("exponent", [0, -133 + 11, 120, -70, -63, -64])
+def test_every_quotient_of_two_numbers(exponent):
+    """for every mantissa of the largest magnitude a row with every mantissa at every exponent that does not round to 0, and both signs"""
+    x = (np.arange(128, 256)[None, :] * 2.0 ** -np.arange(0, 10)[:, None]).ravel()
+    x = np.concatenate([x, -x])
+    rows = np.stack([np.concatenate([np.where(np.abs(x) <= a, x, 0.0), [a] * 16]) for a in range(128, 256)]) * 2.0 ** exponent
+    t = torch.from_numpy(rows).to(torch.bfloat16)
+    n, d = t.shape
+    q, scale = torch.empty((n, d), dtype=torch.int8, device="cuda"), torch.empty(n, device="cuda")
+    B.nanospec_quantize_rows(t.cuda(), n, d, q, scale)
+    eq, es = quantized(t)
+    assert np.array_equal(q.cpu().numpy(), eq) and same(scale.cpu().numpy(), es)
+    # and as hidden rows, by the kernels that round them themselves: an identity matrix gives q back
+    eye = torch.eye(d, dtype=torch.int8, device="cuda")
+    for M in (1, 3, 8, 16):
+        out = torch.empty((M, d), device="cuda")
+        ws, k = workspace(M, d)
+        B.nanospec_dense_head_i8(eye, torch.ones(d, device="cuda"), t[:M].cuda(), d, d, M, out, ws, k)
+        assert same(out.cpu().numpy(), eq[:M].astype(np.float32) * es[:M, None])
+
+
 @pytest.mark.parametrize("V,d", [(1, 16), (17, 48), (100, 256), (1000, 512), (513, 1040), (300, 4096), (5003, 128), (260, 8192)])
 @pytest.mark.parametrize("M", [1, 3, 8, 9, 16, 17, 33, 64, 65, 130, 300])
 def test_dense_logits_to_the_last_bit(V, d, M):
