@@ -76,6 +76,7 @@ hipError_t ensure_device_configured() {
   if (e == hipSuccess) e = hold_configure_device();
   if (e == hipSuccess) e = kslice_configure_device();
   if (e == hipSuccess) e = few_configure_device();
+  if (e == hipSuccess) e = loss_configure_device();
   if (e == hipSuccess) e = packed_configure_device();
   if (e == hipSuccess) g_cfg_done[dev] = true;
   return e;
@@ -515,6 +516,7 @@ nanospec_status nanospec_policy_loss(const nanospec_logit_rows* rows, const floa
   const nanospec_status rc = logit_rows_of(rows, d_workspace, workspace_bytes, &r);
   if (rc != NANOSPEC_OK) return rc;
   if (!grad_ok(r, d_grad, grad_type, ld_grad)) return NANOSPEC_EINVAL;
+  if (ensure_device_configured() != hipSuccess) return NANOSPEC_EHIP;   // a flag test after the first call on the device
   r.weight = d_weight;
   const PolicyArgs a{d_old, kl_beta != 0.f ? d_ref : nullptr, d_adv, clip_low, clip_high, kl_beta, grad_scale, d_loss, d_row_loss, d_logprob};
   return launch_policy_loss(r, a, d_grad, grad_type, ld_grad, static_cast<char*>(d_workspace), static_cast<hipStream_t>(hip_stream)) == hipSuccess ? NANOSPEC_OK

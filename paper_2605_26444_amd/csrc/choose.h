@@ -171,6 +171,13 @@ inline FewPlan few_plan(int32_t M, int32_t d, int32_t batch, int32_t cap_rows, b
   return f;
 }
 
+// ---- losses (loss.hip) --------------------------------------------------------------------------------------------
+
+// Whether a row's loss and gradient are one workgroup's, which reads the row once, or the chip's in pieces, twice (us, fp32 logits to bf16, apart / one workgroup): 128256
+// columns, 128 rows 34.5 / 31.3, 256 64 / 52.5, 300 78 / 79 (the last 44 rows have the chip to themselves), 2048 518 / 341; 32000, 128 15.4 / 14.6, 2048 135 / 91; 8000, 128 11.7 /
+// 10.2, 2048 37 / 35; 1000, 128 12.2 / 12.6, 2048 17.2 / 20.0; 152064, of which 21000 columns are read twice, 2048 612 / 430.
+inline bool policy_fuses(int32_t rows, int32_t V) { return rows >= 128 && V >= 4096; }
+
 // The 8-bit head's block shapes beyond: as many bytes a step hold twice the columns.  256 x 256 blocks with the scales do not fit LDS, so d that is no multiple of 128 takes 256 x 128.
 inline WideShape i8_shape(int32_t M, int32_t d, int32_t batch, int32_t cap_rows, bool dense) {
   const WideShape s = wide_shape(M, d / 2, batch, cap_rows, dense, d % 128 == 0);

@@ -287,6 +287,7 @@ hipError_t launch_head_few_i8(const int8_t* W, const float* W_scale, const void*
                               int32_t cap_rows, int32_t V, int32_t batch, int32_t M, int32_t d, int64_t ld, float* logits, hipStream_t s);
 
 // loss.hip
+hipError_t loss_configure_device();
 int64_t loss_workspace_bytes(int32_t rows, int32_t V);
 hipError_t launch_token_logprob(const LogitRows& r, float* logprob, char* ws, hipStream_t s);
 hipError_t launch_policy_loss(const LogitRows& r, const PolicyArgs& a, void* grad, int32_t grad_type, int64_t ld_grad, char* ws, hipStream_t s);

@@ -15,11 +15,13 @@
 namespace nanospec {
 
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));           // rows start at any element: 16-byte loads at its alignment
+typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
 typedef uint16_t u16x8_any __attribute__((ext_vector_type(8), aligned(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8_any __attribute__((ext_vector_type(8), aligned(2)));
 
-constexpr int kRowThreads = 256;
+constexpr int kRowThreads = 256;         // of a workgroup that takes a piece of a row
+constexpr int kWholeThreads = 1024;      // of one that takes a long row whole
 constexpr float kLog2e = 0x1.715476p+0f, kLog2eRest = 0x1.4ae0c0p-26f, kLn2 = 0.6931471805599453f;   // log2 e in two parts
 
 // x <= 0: off by 2^-24 (2 |x| + 2) of the result at most
@@ -30,21 +32,25 @@ struct Vec;
 template <>
 struct Vec<float> {
   static constexpr int N = 4;
-  static __device__ __forceinline__ void load(const float* p, float (&x)[N]) {
-    const f32x4_any v = *reinterpret_cast<const f32x4_any*>(p);
+  typedef float Raw __attribute__((ext_vector_type(4)));
+  static __device__ __forceinline__ Raw raw(const float* p) { return *reinterpret_cast<const f32x4_any*>(p); }
+  static __device__ __forceinline__ void open(const Raw& v, float (&x)[N]) {
 #pragma unroll
     for (int i = 0; i < N; ++i) x[i] = v[i];
   }
+  static __device__ __forceinline__ void load(const float* p, float (&x)[N]) { open(raw(p), x); }
   static __device__ __forceinline__ float one(const float* p) { return *p; }
 };
 template <>
 struct Vec<uint16_t> {
   static constexpr int N = 8;
-  static __device__ __forceinline__ void load(const uint16_t* p, float (&x)[N]) {
-    const u16x8_any v = *reinterpret_cast<const u16x8_any*>(p);
+  typedef uint32_t Raw __attribute__((ext_vector_type(4)));
+  static __device__ __forceinline__ Raw raw(const uint16_t* p) { return __builtin_bit_cast(Raw, (u16x8)*reinterpret_cast<const u16x8_any*>(p)); }
+  static __device__ __forceinline__ void open(const Raw& v, float (&x)[N]) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = __uint_as_float((uint32_t)v[i] << 16);
+    for (int i = 0; i < N; ++i) x[i] = __uint_as_float(i & 1 ? v[i / 2] & 0xffff0000u : v[i / 2] << 16);
   }
+  static __device__ __forceinline__ void load(const uint16_t* p, float (&x)[N]) { open(raw(p), x); }
   static __device__ __forceinline__ float one(const uint16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
 };
 
@@ -159,8 +165,8 @@ __device__ __forceinline__ bool row_counts(const LogitRows& r, int row) {
 
 // Piece `blockIdx.x % pieces` of row `blockIdx.x / pieces`: maximum and sum of its columns to part[], and the token's column and logit, from
 // the workgroup that has the row's first columns, to at[].  Rows that do not count are not read.
-template <typename T>
-__global__ __launch_bounds__(kRowThreads) void rows_stats_kernel(const LogitRows r, int pieces, int span, Stat* __restrict__ part, Place* __restrict__ at,
+template <typename T, int NT>
+__global__ __launch_bounds__(NT) void rows_stats_kernel(const LogitRows r, int pieces, int span, Stat* __restrict__ part, Place* __restrict__ at,
                                                                  float* __restrict__ logprob) {
   constexpr int N = Vec<T>::N, U = 16 / N;
   const int row = blockIdx.x / pieces, piece = blockIdx.x - row * pieces, tid = threadIdx.x, w = tid >> 6;
@@ -175,13 +181,13 @@ __global__ __launch_bounds__(kRowThreads) void rows_stats_kernel(const LogitRows
   }
   Stat t{-INFINITY, 0.f};
   int c = c0;
-  for (; c + kRowThreads * N * U <= c1; c += kRowThreads * N * U) {
+  for (; c + NT * N * U <= c1; c += NT * N * U) {
     float x[U * N];
 #pragma unroll
-    for (int u = 0; u < U; ++u) Vec<T>::load(z + c + (u * kRowThreads + tid) * N, *reinterpret_cast<float(*)[N]>(&x[u * N]));
+    for (int u = 0; u < U; ++u) Vec<T>::load(z + c + (u * NT + tid) * N, *reinterpret_cast<float(*)[N]>(&x[u * N]));
     take(t, x);
   }
-  for (c += tid * N; c < c1; c += kRowThreads * N) {
+  for (c += tid * N; c < c1; c += NT * N) {
     float x[N];
     if (c + N <= c1) {
       Vec<T>::load(z + c, x);
@@ -192,12 +198,12 @@ __global__ __launch_bounds__(kRowThreads) void rows_stats_kernel(const LogitRows
     take(t, x);
   }
   t = wave_join(t);
-  __shared__ Stat red[kRowThreads / 64];
+  __shared__ Stat red[NT / 64];
   if ((tid & 63) == 0) red[w] = t;
   __syncthreads();
   if (tid) return;
 #pragma unroll
-  for (int i = 1; i < kRowThreads / 64; ++i) t = join(t, red[i]);
+  for (int i = 1; i < NT / 64; ++i) t = join(t, red[i]);
   if (logprob) {                                           // one piece and nothing else asked for
     logprob[row] = (float)log_probability(a, t);
     return;
@@ -229,7 +235,8 @@ __global__ __launch_bounds__(256) void rows_logprob_kernel(int rows, int pieces,
   if (row < rows) logprob[row] = (float)finish_row(row, pieces, part, at).lp;
 }
 
-// sum over a workgroup of 1024 in a fixed order, in thread 0
+// sum over a workgroup of NT in a fixed order, in thread 0
+template <int NT>
 __device__ __forceinline__ double block_sum(double x, double* red) {
 #pragma unroll
   for (int o = 32; o; o >>= 1) x += __shfl_down(x, o);
@@ -237,7 +244,7 @@ __device__ __forceinline__ double block_sum(double x, double* red) {
   __syncthreads();
   double s = 0;
   if (threadIdx.x == 0)
-    for (int i = 0; i < 16; ++i) s += red[i];
+    for (int i = 0; i < NT / 64; ++i) s += red[i];
   return s;
 }
 
@@ -251,66 +258,252 @@ __device__ __forceinline__ RowCoef coef_of(const Stat& t, int col, double c, flo
   return RowCoef{t.m, (float)(-(c * grad_scale) / (double)t.s), (float)(c * grad_scale), col};
 }
 
-__global__ __launch_bounds__(1024) void policy_rows_kernel(const LogitRows r, int pieces, const Stat* __restrict__ part, const Place* __restrict__ at, const PolicyArgs a,
-                                                           RowCoef* __restrict__ coef) {
-  __shared__ double red[16];
+// a row's policy loss and its derivative by the log-probability
+struct PolicyRow {
+  double loss, c;
+};
+
+__device__ __forceinline__ PolicyRow policy_row(const PolicyArgs& a, int row, double lp) {
+  const double adv = a.adv[row], ratio = exp(lp - (double)a.old[row]);
+  const double lo = 1.0 - (double)a.clip_low, hi = 1.0 + (double)a.clip_high;
+  const double held = (ratio < lo ? lo : ratio > hi ? hi : ratio) * adv, free = ratio * adv;
+  PolicyRow r{-(free <= held ? free : held), free <= held ? -free : 0.0};
+  if (free != free) r.loss = r.c = free;                   // NaN stays NaN
+  if (a.ref) {
+    const double gap = (double)a.ref[row] - lp, e = exp(gap);
+    r.loss += (double)a.beta * (e - gap - 1.0);
+    r.c += (double)a.beta * (1.0 - e);
+  }
+  return r;
+}
+
+__device__ __forceinline__ double weight_of(const LogitRows& r, int row) { return r.weight ? (double)r.weight[row] : 1.0; }
+
+// all rows by one workgroup
+template <int NT>
+__device__ void policy_rows(const LogitRows& r, int pieces, const Stat* __restrict__ part, const Place* __restrict__ at, const PolicyArgs& a, RowCoef* __restrict__ coef) {
+  __shared__ double red[NT / 64];
   double sum = 0;
-  for (int row = threadIdx.x; row < r.rows; row += 1024) {
+  for (int row = threadIdx.x; row < r.rows; row += NT) {
     float lp_out = 0.f, loss_out = 0.f;
     RowCoef k{0.f, 0.f, 0.f, -1};
     if (row_counts(r, row)) {
       const RowResult q = finish_row(row, pieces, part, at);
       lp_out = (float)q.lp;
       if (q.has) {
-        const double w = r.weight ? (double)r.weight[row] : 1.0, adv = a.adv[row];
-        const double ratio = exp(q.lp - (double)a.old[row]);
-        const double lo = 1.0 - (double)a.clip_low, hi = 1.0 + (double)a.clip_high;
-        const double held = (ratio < lo ? lo : ratio > hi ? hi : ratio) * adv, free = ratio * adv;
-        double loss = -(free <= held ? free : held), c = free <= held ? -free : 0.0;
-        if (free != free) loss = c = free;                 // NaN stays NaN
-        if (a.ref) {
-          const double gap = (double)a.ref[row] - q.lp, e = exp(gap);
-          loss += (double)a.beta * (e - gap - 1.0);
-          c += (double)a.beta * (1.0 - e);
-        }
-        loss_out = (float)loss;
-        sum += w * loss;
-        k = coef_of(q.t, q.col, w * c, a.grad_scale);
+        const PolicyRow x = policy_row(a, row, q.lp);
+        const double w = weight_of(r, row);
+        loss_out = (float)x.loss;
+        sum += w * x.loss;
+        k = coef_of(q.t, q.col, w * x.c, a.grad_scale);
       }
     }
     if (a.row_loss) a.row_loss[row] = loss_out;
     if (a.logprob) a.logprob[row] = lp_out;
     if (coef) coef[row] = k;
   }
-  sum = block_sum(sum, red);
+  sum = block_sum<NT>(sum, red);
   if (threadIdx.x == 0) a.loss[0] = (float)sum;
 }
 
-// one workgroup; the answers' first rows travel by value
-__global__ __launch_bounds__(1024) void pair_rows_kernel(const LogitRows r, int pieces, const Stat* __restrict__ part, const Place* __restrict__ at, const PairArgs a, const Offsets off,
-                                                         double* __restrict__ term, RowCoef* __restrict__ coef) {
-  __shared__ double red[16], sums[NANOSPEC_MAX_BATCH];
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  for (int row = tid; row < r.rows; row += 1024) {
-    float lp_out = 0.f;
-    double t = 0;
-    RowCoef k{0.f, 0.f, 0.f, -1};
-    if (row_counts(r, row)) {
-      const RowResult q = finish_row(row, pieces, part, at);
-      lp_out = (float)q.lp;
-      if (q.has) {
-        const double wt = r.weight ? (double)r.weight[row] : 1.0;
-        t = wt * (q.lp - (a.ref ? (double)a.ref[row] : 0.0));
-        k = RowCoef{q.t.m, q.t.s, (float)wt, q.col};
+__global__ __launch_bounds__(1024) void policy_rows_kernel(const LogitRows r, int pieces, const Stat* __restrict__ part, const Place* __restrict__ at, const PolicyArgs a,
+                                                           RowCoef* __restrict__ coef) {
+  policy_rows<1024>(r, pieces, part, at, a, coef);
+}
+
+// the rows' weighted losses, added in a fixed order
+__global__ __launch_bounds__(1024) void policy_sum_kernel(int rows, const double* __restrict__ term, float* __restrict__ loss) {
+  __shared__ double red[16];
+  double sum = 0;
+  for (int row = threadIdx.x; row < rows; row += 1024) sum += term[row];
+  sum = block_sum<1024>(sum, red);
+  if (threadIdx.x == 0) loss[0] = (float)sum;
+}
+
+// A row's policy loss and its gradient by one workgroup, which keeps the row on the compute unit between the two: RC pieces of 16 bytes a thread in
+// registers, LC in LDS, so that up to (RC + LC) 8 KB of a row are read from memory once; what is beyond is read a second time, from
+// the caches.  Two launches over all rows instead read them twice from memory (2048 rows of 128256 in fp32: 1 GB).
+// A chunk is what the workgroup's threads hold in a piece each; a row's full chunks go to LDS first, then to registers, the others and the row's end are streamed.
+template <typename T, typename G, int RC, int LC>
+__global__ __launch_bounds__(512, 2) void policy_fused_kernel(const LogitRows r, const PolicyArgs a, double* __restrict__ term, G* __restrict__ grad, int64_t ld_grad) {
+  constexpr int N = Vec<T>::N, CH = 512 * N, U = 16 / N;                  // U pieces: 16 numbers, what a step of the sums takes
+  static_assert(RC % U == 0 && LC % U == 0 && LC <= RC, "whole steps");
+  typedef typename Vec<T>::Raw Raw;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  __shared__ Stat red[8];
+  __shared__ RowCoef shared_k;
+  __shared__ float shared_z;
+  Raw* held = reinterpret_cast<Raw*>(smem);                               // [LC][512]
+  const int row = blockIdx.x, tid = threadIdx.x, w = tid >> 6;
+  const T* z = static_cast<const T*>(r.z) + (int64_t)row * r.ld;
+  G* g = grad + (int64_t)row * ld_grad;
+  const int n = row_columns(r, row);
+  const int full = n / CH;
+  if (!row_counts(r, row)) {
+    const float x[N] = {};
+    for (int c = tid * N; c < n; c += CH) {
+      if (c + N <= n) store_vec(g + c, x);
+      else
+        for (int i = c; i < n; ++i) store_one(g + i, 0.f);
+    }
+    if (tid == 0) {
+      if (a.row_loss) a.row_loss[row] = 0.f;
+      if (a.logprob) a.logprob[row] = 0.f;
+      term[row] = 0;
+    }
+    return;
+  }
+  // chunks: LDS 0 .. nl - 1, registers nl .. nl + nr - 1, streamed from there on
+  const int nl = full < LC ? full / U * U : LC, nr = full - nl < RC ? (full - nl) / U * U : RC, from = nl + nr;
+  Stat t{-INFINITY, 0.f};
+  Raw v[RC];
+  const T* zt = z + tid * N;
+  // a load past the chunks there are is the last one's again: the number of loads in flight does not depend on the row
+  auto chunk = [&](int c) { return Vec<T>::raw(zt + (int64_t)(c < from ? c : from - 1) * CH); };
+  Place pl{-INFINITY, -1};
+  if (from) {
+#pragma unroll
+    for (int c = 0; c < RC; ++c) v[c] = chunk(c < LC && LC ? (nl ? c : nl + c) : nl + c);
+  }
+  if (w == 0) {
+    pl.col = token_column(r, row, n);
+    if (pl.col >= 0) pl.z = Vec<T>::one(z + pl.col);
+  }
+  if (from) {
+    if (LC && nl) {
+#pragma unroll
+      for (int c = 0; c < LC; c += U) {
+        if (c < nl) {
+          float x[16];
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            held[(c + u) * 512 + tid] = v[c + u];
+            Vec<T>::open(v[c + u], *reinterpret_cast<float(*)[N]>(&x[u * N]));
+          }
+          take(t, x);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[c + u] = chunk(nl + c + u);
       }
     }
-    if (a.logprob) a.logprob[row] = lp_out;
-    term[row] = t;
-    if (coef) coef[row] = k;
+#pragma unroll
+    for (int c = 0; c < RC; c += U) {
+      if (c < nr) {
+        float x[16];
+#pragma unroll
+        for (int u = 0; u < U; ++u) Vec<T>::open(v[c + u], *reinterpret_cast<float(*)[N]>(&x[u * N]));
+        take(t, x);
+      }
+    }
+  }
+  for (int c = from * CH + tid * N; c < n; c += CH) {
+    float x[N];
+    if (c + N <= n) {
+      Vec<T>::load(z + c, x);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] = c + i < n ? Vec<T>::one(z + c + i) : -INFINITY;
+    }
+    take(t, x);
+  }
+  t = wave_join(t);
+  if ((tid & 63) == 0) red[w] = t;
+  __syncthreads();
+  if (tid == 0) {
+#pragma unroll
+    for (int i = 1; i < 8; ++i) t = join(t, red[i]);
+    const double lp = log_probability(pl, t);
+    RowCoef k{0.f, 0.f, 0.f, -1};
+    double loss = 0, sum = 0;
+    if (!(lp < -745.0)) {
+      const PolicyRow x = policy_row(a, row, lp);
+      const double wt = weight_of(r, row);
+      loss = x.loss;
+      sum = wt * x.loss;
+      k = coef_of(t, pl.col, wt * x.c, a.grad_scale);
+    }
+    if (a.row_loss) a.row_loss[row] = (float)loss;
+    if (a.logprob) a.logprob[row] = (float)lp;
+    term[row] = sum;
+    shared_k = k;
+    shared_z = pl.z;
+  }
+  __syncthreads();
+  const RowCoef k = shared_k;
+  auto value = [&](float x) { return k.c == 0.f ? 0.f : k.scale * exp_neg(x - k.m); };
+  G* gt = g + tid * N;
+  auto put = [&](int c, const Raw& y) {
+    float x[N];
+    Vec<T>::open(y, x);
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = value(x[i]);
+    store_vec(gt + (int64_t)c * CH, x);
+  };
+#pragma unroll
+  for (int c = 0; c < RC; ++c)
+    if (c < nr) put(nl + c, v[c]);
+  for (int c = 0; c < nl; ++c) put(c, held[c * 512 + tid]);
+  for (int c = from * CH + tid * N; c < n; c += CH) {
+    if (c + N <= n) {
+      put(c / CH, Vec<T>::raw(z + c));
+    } else {
+      for (int i = c; i < n; ++i) store_one(g + i, value(Vec<T>::one(z + i)));
+    }
+  }
+  // the token's own entry, by the thread that has just written its column
+  if (k.c != 0.f && tid == k.col % CH / N) store_one(g + k.col, value(shared_z) + k.c);
+}
+
+// a pair's loss and its derivative by the margin
+struct PairLoss {
+  double loss, slope;
+};
+
+__device__ __forceinline__ PairLoss pair_loss(const PairArgs& a, double margin) {
+  const double e = (double)a.smoothing, less = log1p(exp(-fabs(margin)));               // log(1 + exp(-m)) = max(-m, 0) + less
+  const double up = 1.0 / (1.0 + exp(margin)), down = 1.0 / (1.0 + exp(-margin));       // sigma(-m), sigma(m)
+  PairLoss p{(1.0 - e) * (fmax(-margin, 0.0) + less) + e * (fmax(margin, 0.0) + less), (1.0 - e) * -up + e * down};
+  if (margin != margin) p.loss = margin;
+  return p;
+}
+
+// what a row adds to its answer's sum
+__device__ __forceinline__ double pair_term(const LogitRows& r, const PairArgs& a, int row, const RowResult& q) {
+  return q.has ? weight_of(r, row) * (q.lp - (a.ref ? (double)a.ref[row] : 0.0)) : 0.0;
+}
+
+// the derivative by a row's log-probability, from that by its pair's margin; rejected: the second answer of the pair
+__device__ __forceinline__ double pair_coef(const LogitRows& r, const PairArgs& a, int row, double slope, bool rejected) {
+  return (rejected ? -1.0 : 1.0) * slope * ((double)a.beta / a.pairs) * weight_of(r, row);
+}
+
+// the answer that holds a row: off[lo] <= row < off[lo + 1]
+__device__ __forceinline__ int answer_of(const Offsets& off, int pairs, int row) {
+  int lo = 0, hi = 2 * pairs;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (off.v[mid] <= row) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+// all rows by one workgroup
+template <int NT>
+__device__ void pair_rows(const LogitRows& r, int pieces, const Stat* __restrict__ part, const Place* __restrict__ at, const PairArgs& a, const Offsets& off,
+                          double* __restrict__ term, RowCoef* __restrict__ coef) {
+  __shared__ double red[NT / 64], sums[NANOSPEC_MAX_BATCH];
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  for (int row = tid; row < r.rows; row += NT) {
+    RowResult q{};
+    const bool counts = row_counts(r, row);
+    if (counts) q = finish_row(row, pieces, part, at);
+    if (a.logprob) a.logprob[row] = counts ? (float)q.lp : 0.f;
+    term[row] = counts ? pair_term(r, a, row, q) : 0.0;
   }
   __threadfence_block();
   __syncthreads();
-  for (int q = w; q < 2 * a.pairs; q += 16) {              // a wavefront an answer
+  for (int q = w; q < 2 * a.pairs; q += NT / 64) {         // a wavefront an answer
     double s = 0;
     for (int row = off.v[q] + lane; row < off.v[q + 1]; row += 64) s += term[row];
 #pragma unroll
@@ -318,47 +511,39 @@ __global__ __launch_bounds__(1024) void pair_rows_kernel(const LogitRows r, int 
     if (lane == 0) sums[q] = s;
   }
   __syncthreads();
-  double loss = 0, slope = 0;
+  PairLoss p{0, 0};
   if (tid < a.pairs) {
-    const double margin = (double)a.beta * (sums[2 * tid] - sums[2 * tid + 1]), e = (double)a.smoothing;
-    const double less = log1p(exp(-fabs(margin)));         // log(1 + exp(-m)) = max(-m, 0) + less
-    loss = (1.0 - e) * (fmax(-margin, 0.0) + less) + e * (fmax(margin, 0.0) + less);
-    if (margin != margin) loss = margin;
-    const double up = 1.0 / (1.0 + exp(margin)), down = 1.0 / (1.0 + exp(-margin));   // sigma(-m), sigma(m)
-    slope = ((1.0 - e) * -up + e * down) * (double)a.beta / a.pairs;
+    const double margin = (double)a.beta * (sums[2 * tid] - sums[2 * tid + 1]);
+    p = pair_loss(a, margin);
     if (a.margin) a.margin[tid] = (float)margin;
   }
   __syncthreads();
-  if (tid < a.pairs) sums[tid] = slope;
-  loss = block_sum(loss, red);                             // and a barrier behind sums[]
+  if (tid < a.pairs) sums[tid] = p.slope;
+  const double loss = block_sum<NT>(p.loss, red);          // and a barrier behind sums[]
   if (tid == 0) a.loss[0] = (float)(loss / a.pairs);
   if (!coef) return;
-  for (int row = tid; row < r.rows; row += 1024) {
-    const RowCoef k = coef[row];                           // written by this thread
-    RowCoef out{0.f, 0.f, 0.f, -1};
-    if (k.col >= 0) {
-      int lo = 0, hi = 2 * a.pairs;                        // the answer that holds the row: off[lo] <= row < off[lo + 1]
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (off.v[mid] <= row) lo = mid;
-        else hi = mid;
-      }
-      out = coef_of(Stat{k.m, k.scale}, k.col, (lo & 1 ? -1.0 : 1.0) * sums[lo >> 1] * (double)k.c, a.grad_scale);
+  for (int row = tid; row < r.rows; row += NT) {
+    RowCoef k{0.f, 0.f, 0.f, -1};
+    if (row_counts(r, row)) {
+      const RowResult q = finish_row(row, pieces, part, at);
+      const int answer = answer_of(off, a.pairs, row);
+      if (q.has) k = coef_of(q.t, q.col, pair_coef(r, a, row, sums[answer >> 1], answer & 1), a.grad_scale);
     }
-    coef[row] = out;
+    coef[row] = k;
   }
 }
 
-// dL/dz of piece `blockIdx.x % pieces` of a row
+// the answers' first rows travel by value
+__global__ __launch_bounds__(1024) void pair_rows_kernel(const LogitRows r, int pieces, const Stat* __restrict__ part, const Place* __restrict__ at, const PairArgs a, const Offsets off,
+                                                         double* __restrict__ term, RowCoef* __restrict__ coef) {
+  pair_rows<1024>(r, pieces, part, at, a, off, term, coef);
+}
+
+// dL/dz of the columns c0 .. c1 - 1 of a row; z may be the gradient's own memory: every element is read by the thread that writes it
 template <typename T, typename G>
-__global__ __launch_bounds__(kRowThreads) void rows_grad_kernel(const LogitRows r, int pieces, int span, const RowCoef* __restrict__ coef, G* __restrict__ grad, int64_t ld_grad) {
+__device__ __forceinline__ void grad_piece(const T* z, G* g, const RowCoef& k, int c0, int c1) {
   constexpr int N = Vec<T>::N, U = 16 / N;
-  const int row = blockIdx.x / pieces, piece = blockIdx.x - row * pieces, tid = threadIdx.x;
-  const T* z = static_cast<const T*>(r.z) + (int64_t)row * r.ld;     // may be the gradient's own memory: every element is read by the thread that writes it
-  G* g = grad + (int64_t)row * ld_grad;
-  const RowCoef k = coef[row];
-  const int n = row_columns(r, row);
-  const int c0 = piece * span, c1 = c0 + span < n ? c0 + span : n;
+  const int tid = threadIdx.x;
   if (k.c == 0.f) {
     for (int c = c0 + tid * N; c < c1; c += kRowThreads * N) {
       const float x[N] = {};
@@ -398,9 +583,71 @@ __global__ __launch_bounds__(kRowThreads) void rows_grad_kernel(const LogitRows 
   }
 }
 
+// piece `blockIdx.x % pieces` of a row, the last rows first: of those the caches may still hold logits from the pass before (1021 rows of 152064 in bf16: 191 us for 194)
+template <typename T, typename G>
+__global__ __launch_bounds__(kRowThreads) void rows_grad_kernel(const LogitRows r, int pieces, int span, const RowCoef* __restrict__ coef, G* grad, int64_t ld_grad) {
+  const int up = blockIdx.x / pieces, row = r.rows - 1 - up, piece = blockIdx.x - up * pieces;
+  const int n = row_columns(r, row), c0 = piece * span, c1 = c0 + span < n ? c0 + span : n;
+  grad_piece(static_cast<const T*>(r.z) + (int64_t)row * r.ld, grad + (int64_t)row * ld_grad, coef[row], c0, c1);
+}
+
+__device__ __forceinline__ void few_rows_total(const LogitRows& r, int pieces, const Stat* part, const Place* at, const PolicyArgs& a, double*) {
+  policy_rows<kRowThreads>(r, pieces, part, at, a, nullptr);
+}
+
+__device__ __forceinline__ double few_rows_coef(const LogitRows& r, int, const Stat*, const Place*, const PolicyArgs& a, int row, const RowResult& q, double*) {
+  return weight_of(r, row) * policy_row(a, row, q.lp).c;
+}
+
+struct PairFew : PairArgs {
+  Offsets off;
+};
+
+__device__ __forceinline__ void few_rows_total(const LogitRows& r, int pieces, const Stat* part, const Place* at, const PairFew& a, double* term) {
+  pair_rows<kRowThreads>(r, pieces, part, at, a, a.off, term, nullptr);
+}
+
+// every thread a row of the pair, at most kRowThreads of them
+__device__ __forceinline__ double few_rows_coef(const LogitRows& r, int pieces, const Stat* part, const Place* at, const PairFew& a, int row, const RowResult&, double* red) {
+  const int answer = answer_of(a.off, a.pairs, row), first = a.off.v[answer & ~1], mid = a.off.v[answer | 1], last = a.off.v[(answer | 1) + 1];
+  const int mine = first + (int)threadIdx.x;
+  double s = 0;
+  if (mine < last && row_counts(r, mine)) s = (mine < mid ? 1.0 : -1.0) * pair_term(r, a, mine, finish_row(mine, pieces, part, at));
+  s = block_sum<kRowThreads>(s, red);
+  return pair_coef(r, a, row, pair_loss(a, (double)a.beta * s).slope, answer & 1);       // of thread 0 only
+}
+
+// Few rows: the coefficients by every workgroup for itself, from the pieces' sums, in the launch that writes the gradient, and the totals by one workgroup more: a
+// launch less.
+template <typename T, typename G, typename A>
+__global__ __launch_bounds__(kRowThreads) void few_rows_grad_kernel(const LogitRows r, int pieces, int span, const Stat* part, const Place* at, const A a, double* term, G* grad,
+                                                                    int64_t ld_grad) {
+  __shared__ double red[kRowThreads / 64];
+  __shared__ RowCoef shared_k;
+  if ((int)blockIdx.x == r.rows * pieces) {
+    few_rows_total(r, pieces, part, at, a, term);
+    return;
+  }
+  const int row = blockIdx.x / pieces, piece = blockIdx.x - row * pieces;
+  const int n = row_columns(r, row), c0 = piece * span, c1 = c0 + span < n ? c0 + span : n;
+  if (c0 >= c1) return;
+  RowCoef k{0.f, 0.f, 0.f, -1};
+  if (row_counts(r, row)) {
+    const RowResult q = finish_row(row, pieces, part, at);
+    const double c = few_rows_coef(r, pieces, part, at, a, row, q, red);
+    if (threadIdx.x == 0) shared_k = q.has ? coef_of(q.t, q.col, c, a.grad_scale) : k;
+    __syncthreads();
+    k = shared_k;
+  }
+  grad_piece(static_cast<const T*>(r.z) + (int64_t)row * r.ld, grad + (int64_t)row * ld_grad, k, c0, c1);
+}
+
 // ---- host --------------------------------------------------------------------------------------------------------
 
-// Rows cut into pieces until there are 2048 workgroups (eight a compute unit), of no less than 4096 columns, a multiple of what a pass of a workgroup takes.
+// Long rows, a workgroup for every compute unit at least: whole rows (509 x 128256 in fp32: 
+// Else rows cut into pieces until there are 2048 workgroups (eight a compute unit), of no less than 4096 columns, a multiple of what a pass of a workgroup takes.
+static bool whole_rows(int32_t rows, int32_t V) { return rows >= 256 && V >= 16384; }
+
 static RowCut row_cut(int32_t rows, int32_t V) {
   int64_t pieces = (2048 + rows - 1) / rows;
   const int64_t most = (V + 4095) / 4096;
@@ -408,6 +655,8 @@ static RowCut row_cut(int32_t rows, int32_t V) {
   const int64_t span = ((V + pieces - 1) / pieces + 4095) / 4096 * 4096;
   return RowCut{(int32_t)((V + span - 1) / span), (int32_t)(span < V ? span : V)};
 }
+
+static RowCut stats_cut(int32_t rows, int32_t V) { return whole_rows(rows, V) ? RowCut{1, V} : row_cut(rows, V); }
 
 static int64_t up256(int64_t x) { return (x + 255) / 256 * 256; }
 
@@ -436,13 +685,17 @@ int64_t loss_workspace_bytes(int32_t rows, int32_t V) {
 }
 
 static hipError_t run_stats(const LogitRows& r, const LossSpace& s, float* logprob, hipStream_t stream) {
-  const RowCut cut = row_cut(r.rows, r.V);
-  const int64_t grid = (int64_t)r.rows * cut.pieces;
-  if (grid > 0x7fffffff) return hipErrorInvalidValue;
-  if (r.type == NANOSPEC_F32)
-    rows_stats_kernel<float><<<dim3((unsigned)grid), kRowThreads, 0, stream>>>(r, cut.pieces, cut.span, s.part, s.at, logprob);
-  else
-    rows_stats_kernel<uint16_t><<<dim3((unsigned)grid), kRowThreads, 0, stream>>>(r, cut.pieces, cut.span, s.part, s.at, logprob);
+  const RowCut cut = stats_cut(r.rows, r.V);
+  const unsigned grid = (unsigned)((int64_t)r.rows * cut.pieces);
+#define NS_STATS(T, NT) rows_stats_kernel<T, NT><<<dim3(grid), NT, 0, stream>>>(r, cut.pieces, cut.span, s.part, s.at, logprob)
+  if (whole_rows(r.rows, r.V)) {
+    if (r.type == NANOSPEC_F32) NS_STATS(float, kWholeThreads);
+    else NS_STATS(uint16_t, kWholeThreads);
+  } else {
+    if (r.type == NANOSPEC_F32) NS_STATS(float, kRowThreads);
+    else NS_STATS(uint16_t, kRowThreads);
+  }
+#undef NS_STATS
   return hipGetLastError();
 }
 
@@ -461,20 +714,74 @@ static hipError_t run_grad(const LogitRows& r, const LossSpace& s, void* grad, i
   return hipGetLastError();
 }
 
+// few rows: see few_rows_grad_kernel; a thread for every row of a pair
+static bool few_rows(int32_t rows) { return rows <= 128; }
+
+template <typename A>
+static hipError_t run_few_rows(const LogitRows& r, const LossSpace& s, const A& a, void* grad, int32_t type, int64_t ld, hipStream_t stream) {
+  const RowCut cut = stats_cut(r.rows, r.V);
+  const unsigned grid = (unsigned)(r.rows * cut.pieces) + 1;
+#define NS_FEW(T, G) few_rows_grad_kernel<T, G, A><<<dim3(grid), kRowThreads, 0, stream>>>(r, cut.pieces, cut.span, s.part, s.at, a, s.term, static_cast<G*>(grad), ld)
+  if (r.type == NANOSPEC_F32) {
+    if (type == NANOSPEC_F32) NS_FEW(float, float);
+    else NS_FEW(float, uint16_t);
+  } else {
+    if (type == NANOSPEC_F32) NS_FEW(uint16_t, float);
+    else NS_FEW(uint16_t, uint16_t);
+  }
+#undef NS_FEW
+  return hipGetLastError();
+}
+
 hipError_t launch_token_logprob(const LogitRows& r, float* logprob, char* ws, hipStream_t stream) {
   const LossSpace s = loss_space(ws, r.rows, r.V);
-  const int pieces = row_cut(r.rows, r.V).pieces;
+  const int pieces = stats_cut(r.rows, r.V).pieces;
   hipError_t e = run_stats(r, s, pieces == 1 ? logprob : nullptr, stream);
   if (e != hipSuccess || pieces == 1) return e;
   rows_logprob_kernel<<<dim3((unsigned)((r.rows + 255) / 256)), 256, 0, stream>>>(r.rows, pieces, s.part, s.at, logprob);
   return hipGetLastError();
 }
 
+// Chunks of 8 KB a row: what a workgroup of policy_fused_kernel holds.
+template <typename T, typename G>
+static hipError_t run_policy_fused(const LogitRows& r, const PolicyArgs& a, double* term, void* grad, int64_t ld_grad, hipStream_t s) {
+  const int64_t bytes = (int64_t)r.V * sizeof(T);
+  G* g = static_cast<G*>(grad);
+  if (bytes <= 16 * 8192) policy_fused_kernel<T, G, 16, 0><<<dim3((unsigned)r.rows), 512, 0, s>>>(r, a, term, g, ld_grad);
+  else if (bytes <= 32 * 8192) policy_fused_kernel<T, G, 32, 0><<<dim3((unsigned)r.rows), 512, 0, s>>>(r, a, term, g, ld_grad);
+  else policy_fused_kernel<T, G, 48, 16><<<dim3((unsigned)r.rows), 512, 16 * 8192, s>>>(r, a, term, g, ld_grad);
+  return hipGetLastError();
+}
+
+template <typename T, typename G>
+static hipError_t configure_policy() {
+  return hipFuncSetAttribute(reinterpret_cast<const void*>(policy_fused_kernel<T, G, 48, 16>), hipFuncAttributeMaxDynamicSharedMemorySize, 16 * 8192);
+}
+
+hipError_t loss_configure_device() {
+  hipError_t e = configure_policy<float, float>();
+  if (e == hipSuccess) e = configure_policy<float, uint16_t>();
+  if (e == hipSuccess) e = configure_policy<uint16_t, float>();
+  if (e == hipSuccess) e = configure_policy<uint16_t, uint16_t>();
+  return e;
+}
+
+static hipError_t launch_policy_fused(const LogitRows& r, const PolicyArgs& a, double* term, void* grad, int32_t type, int64_t ld, hipStream_t s) {
+  hipError_t e;
+  if (r.type == NANOSPEC_F32) e = type == NANOSPEC_F32 ? run_policy_fused<float, float>(r, a, term, grad, ld, s) : run_policy_fused<float, uint16_t>(r, a, term, grad, ld, s);
+  else e = type == NANOSPEC_F32 ? run_policy_fused<uint16_t, float>(r, a, term, grad, ld, s) : run_policy_fused<uint16_t, uint16_t>(r, a, term, grad, ld, s);
+  if (e != hipSuccess) return e;
+  policy_sum_kernel<<<dim3(1), 1024, 0, s>>>(r.rows, term, a.loss);
+  return hipGetLastError();
+}
+
 hipError_t launch_policy_loss(const LogitRows& r, const PolicyArgs& a, void* grad, int32_t grad_type, int64_t ld_grad, char* ws, hipStream_t stream) {
   const LossSpace s = loss_space(ws, r.rows, r.V);
+  if (grad && policy_fuses(r.rows, r.V)) return launch_policy_fused(r, a, s.term, grad, grad_type, ld_grad, stream);
   hipError_t e = run_stats(r, s, nullptr, stream);
   if (e != hipSuccess) return e;
-  policy_rows_kernel<<<dim3(1), 1024, 0, stream>>>(r, row_cut(r.rows, r.V).pieces, s.part, s.at, a, grad ? s.coef : nullptr);
+  if (grad && few_rows(r.rows)) return run_few_rows(r, s, a, grad, grad_type, ld_grad, stream);
+  policy_rows_kernel<<<dim3(1), 1024, 0, stream>>>(r, stats_cut(r.rows, r.V).pieces, s.part, s.at, a, grad ? s.coef : nullptr);
   e = hipGetLastError();
   return e == hipSuccess && grad ? run_grad(r, s, grad, grad_type, ld_grad, stream) : e;
 }
@@ -483,7 +790,8 @@ hipError_t launch_preference_loss(const LogitRows& r, const PairArgs& a, const O
   const LossSpace s = loss_space(ws, r.rows, r.V);
   hipError_t e = run_stats(r, s, nullptr, stream);
   if (e != hipSuccess) return e;
-  pair_rows_kernel<<<dim3(1), 1024, 0, stream>>>(r, row_cut(r.rows, r.V).pieces, s.part, s.at, a, off, s.term, grad ? s.coef : nullptr);
+  if (grad && few_rows(r.rows)) return run_few_rows(r, s, PairFew{a, off}, grad, grad_type, ld_grad, stream);
+  pair_rows_kernel<<<dim3(1), 1024, 0, stream>>>(r, stats_cut(r.rows, r.V).pieces, s.part, s.at, a, off, s.term, grad ? s.coef : nullptr);
   e = hipGetLastError();
   return e == hipSuccess && grad ? run_grad(r, s, grad, grad_type, ld_grad, stream) : e;
 }
