@@ -21,7 +21,6 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8_any __attribute__((ext_vector_type(8), aligned(2)));
 
 constexpr int kRowThreads = 256;         // of a workgroup that takes a piece of a row
-constexpr int kWholeThreads = 1024;      // of one that takes a long row whole
 constexpr float kLog2e = 0x1.715476p+0f, kLog2eRest = 0x1.4ae0c0p-26f, kLn2 = 0.6931471805599453f;   // log2 e in two parts
 
 // x <= 0: off by 2^-24 (2 |x| + 2) of the result at most
@@ -168,7 +167,7 @@ __device__ __forceinline__ bool row_counts(const LogitRows& r, int row) {
 template <typename T, int NT>
 __global__ __launch_bounds__(NT) void rows_stats_kernel(const LogitRows r, int pieces, int span, Stat* __restrict__ part, Place* __restrict__ at,
                                                                  float* __restrict__ logprob) {
-  constexpr int N = Vec<T>::N, U = 16 / N;
+  constexpr int N = Vec<T>::N;
   const int row = blockIdx.x / pieces, piece = blockIdx.x - row * pieces, tid = threadIdx.x, w = tid >> 6;
   if (!row_counts(r, row)) return;
   const T* z = static_cast<const T*>(r.z) + (int64_t)row * r.ld;
@@ -179,22 +178,58 @@ __global__ __launch_bounds__(NT) void rows_stats_kernel(const LogitRows r, int p
     a.col = token_column(r, row, n);
     if (a.col >= 0) a.z = Vec<T>::one(z + a.col);
   }
+  // whole steps of four pieces of 16 bytes a thread, the next step's on their way while one is taken
+  constexpr int U = 4, STEP = NT * N * U;
+  typedef typename Vec<T>::Raw Raw;
   Stat t{-INFINITY, 0.f};
   int c = c0;
-  for (; c + NT * N * U <= c1; c += NT * N * U) {
-    float x[U * N];
+  if (c0 + STEP <= c1) {
+    Raw v[2][U];
+    auto fetch = [&](int b, int at) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) Vec<T>::load(z + c + (u * NT + tid) * N, *reinterpret_cast<float(*)[N]>(&x[u * N]));
-    take(t, x);
-  }
-  for (c += tid * N; c < c1; c += NT * N) {
-    float x[N];
-    if (c + N <= c1) {
-      Vec<T>::load(z + c, x);
-    } else {
+      for (int u = 0; u < U; ++u) v[b][u] = Vec<T>::raw(z + at + (u * NT + tid) * N);
+    };
+    auto use = [&](int b) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) x[i] = c + i < c1 ? Vec<T>::one(z + c + i) : -INFINITY;
+      for (int u = 0; u < U; u += 16 / N) {
+        float x[16];
+#pragma unroll
+        for (int i = 0; i < 16 / N; ++i) Vec<T>::open(v[b][u + i], *reinterpret_cast<float(*)[N]>(&x[i * N]));
+        take(t, x);
+      }
+    };
+    const int steps = (c1 - c0) / STEP, last = c0 + (steps - 1) * STEP;    // past the end the last step again, not used
+    fetch(0, c0);
+    for (int i = 0; i < steps; i += 2) {
+      fetch(1, c + STEP < last ? c + STEP : last);
+      __builtin_amdgcn_sched_barrier(0);
+      use(0);
+      fetch(0, c + 2 * STEP < last ? c + 2 * STEP : last);
+      __builtin_amdgcn_sched_barrier(0);
+      if (i + 1 < steps) use(1);
+      c += 2 * STEP;
     }
+    c = last + STEP;
+  }
+  // the rest, less than a step: its loads go out together as well
+  if (c < c1) {
+    const int whole = (c1 - c) / N * N;
+    Raw v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int at = (u * NT + tid) * N;
+      if (u * NT * N < whole) v[u] = Vec<T>::raw(z + c + (at < whole ? at : 0));
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (u * NT * N >= whole) break;
+      float x[N];
+      Vec<T>::open(v[u], x);
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] = (u * NT + tid) * N < whole ? x[i] : -INFINITY;
+      take(t, x);
+    }
+    const float x[1] = {tid < c1 - c - whole ? Vec<T>::one(z + c + whole + tid) : -INFINITY};
     take(t, x);
   }
   t = wave_join(t);
@@ -500,6 +535,7 @@ __device__ void pair_rows(const LogitRows& r, int pieces, const Stat* __restrict
     if (counts) q = finish_row(row, pieces, part, at);
     if (a.logprob) a.logprob[row] = counts ? (float)q.lp : 0.f;
     term[row] = counts ? pair_term(r, a, row, q) : 0.0;
+    if (coef) coef[row] = RowCoef{q.t.m, q.t.s, 0.f, q.has ? q.col : -1};  // the coefficient follows
   }
   __threadfence_block();
   __syncthreads();
@@ -522,12 +558,11 @@ __device__ void pair_rows(const LogitRows& r, int pieces, const Stat* __restrict
   const double loss = block_sum<NT>(p.loss, red);          // and a barrier behind sums[]
   if (tid == 0) a.loss[0] = (float)(loss / a.pairs);
   if (!coef) return;
-  for (int row = tid; row < r.rows; row += NT) {
-    RowCoef k{0.f, 0.f, 0.f, -1};
-    if (row_counts(r, row)) {
-      const RowResult q = finish_row(row, pieces, part, at);
+  for (int row = tid; row < r.rows; row += NT) {           // written by this thread above
+    RowCoef k = coef[row];
+    if (k.col >= 0) {
       const int answer = answer_of(off, a.pairs, row);
-      if (q.has) k = coef_of(q.t, q.col, pair_coef(r, a, row, sums[answer >> 1], answer & 1), a.grad_scale);
+      k = coef_of(Stat{k.m, k.scale}, k.col, pair_coef(r, a, row, sums[answer >> 1], answer & 1), a.grad_scale);
     }
     coef[row] = k;
   }
@@ -644,9 +679,11 @@ __global__ __launch_bounds__(kRowThreads) void few_rows_grad_kernel(const LogitR
 
 // ---- host --------------------------------------------------------------------------------------------------------
 
-// Long rows, a workgroup for every compute unit at least: whole rows (509 x 128256 in fp32: 
-// Else rows cut into pieces until there are 2048 workgroups (eight a compute unit), of no less than 4096 columns, a multiple of what a pass of a workgroup takes.
-static bool whole_rows(int32_t rows, int32_t V) { return rows >= 256 && V >= 16384; }
+// Threads of a workgroup that takes a whole row, where there are rows for half the compute units; 0: rows are cut into pieces until there are 2048 workgroups of
+// kRowThreads, of no less than 4096 columns, and joined by a launch of its own (us, pieces / 256 / 512 / 1024 threads: 128 rows of 128256 in fp32 16.7 / 15.8 / 14.5 / 16.0, 509
+// 53.8 / 53.4 / 53.1 / 52.5, 1021 of 152064 in bf16 67.5 / 66.1 / 64.6 / 63.2, 1500 of 17000 28.9 / 22.4 / 23.6 / 30.0, 3000 of 32000 in bf16 41.2 / 41.6 / 41.5 / 48.6; 300 of 128256,
+// whose last 44 rows have the chip to themselves, 35 / 38 / 40 / 41).
+static int whole_threads(int32_t rows, int32_t V) { return rows < 128 || V < 16384 ? 0 : V < 32768 ? 256 : 512; }
 
 static RowCut row_cut(int32_t rows, int32_t V) {
   int64_t pieces = (2048 + rows - 1) / rows;
@@ -656,7 +693,7 @@ static RowCut row_cut(int32_t rows, int32_t V) {
   return RowCut{(int32_t)((V + span - 1) / span), (int32_t)(span < V ? span : V)};
 }
 
-static RowCut stats_cut(int32_t rows, int32_t V) { return whole_rows(rows, V) ? RowCut{1, V} : row_cut(rows, V); }
+static RowCut stats_cut(int32_t rows, int32_t V) { return whole_threads(rows, V) ? RowCut{1, V} : row_cut(rows, V); }
 
 static int64_t up256(int64_t x) { return (x + 255) / 256 * 256; }
 
@@ -688,13 +725,16 @@ static hipError_t run_stats(const LogitRows& r, const LossSpace& s, float* logpr
   const RowCut cut = stats_cut(r.rows, r.V);
   const unsigned grid = (unsigned)((int64_t)r.rows * cut.pieces);
 #define NS_STATS(T, NT) rows_stats_kernel<T, NT><<<dim3(grid), NT, 0, stream>>>(r, cut.pieces, cut.span, s.part, s.at, logprob)
-  if (whole_rows(r.rows, r.V)) {
-    if (r.type == NANOSPEC_F32) NS_STATS(float, kWholeThreads);
-    else NS_STATS(uint16_t, kWholeThreads);
-  } else {
-    if (r.type == NANOSPEC_F32) NS_STATS(float, kRowThreads);
-    else NS_STATS(uint16_t, kRowThreads);
+#define NS_STATS_T(NT)                                   \
+  do {                                                   \
+    if (r.type == NANOSPEC_F32) NS_STATS(float, NT);     \
+    else NS_STATS(uint16_t, NT);                         \
+  } while (0)
+  switch (whole_threads(r.rows, r.V)) {
+    case 512: NS_STATS_T(512); break;
+    default: NS_STATS_T(kRowThreads);
   }
+#undef NS_STATS_T
 #undef NS_STATS
   return hipGetLastError();
 }
