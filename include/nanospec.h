@@ -311,8 +311,8 @@ NANOSPEC_API nanospec_status nanospec_dense_topk_static(const float* d_logits, i
  *   d_workspace : device scratch of at least nanospec_head_i8_workspace(rows, d) bytes, rows = M_total or batch * M (-1: sizes out
  *                 of range), 256-byte aligned; asked for whatever the sizes.  Calls that may overlap (two streams, two captured
  *                 graphs) must not share one.
- * Limits: d a multiple of 16 and at most 133136 (the sum fits 32 bits); V * d and rows * d below 2^32; d_W_i8, d_Q, d_H_bf16
- * and d_X_bf16 16-byte aligned.
+ * Limits: d a multiple of 16 and at most 133136 (the sum fits 32 bits); V * d and rows * d below 2^32; at most 2^24 hidden rows;
+ * d_W_i8, d_Q, d_H_bf16 and d_X_bf16 16-byte aligned.
  * Errors: EINVAL (null, sizes < 1, a limit exceeded), ECAPACITY (M > m_cap, workspace too small), EHIP.  Asynchronous. */
 NANOSPEC_API nanospec_status nanospec_quantize_rows(const void* d_X_bf16, int64_t rows, int32_t d, int8_t* d_Q, float* d_scale,
                                                     void* hip_stream);
@@ -367,10 +367,10 @@ typedef struct nanospec_logit_rows {
  *   d_loss fp32 [1]; d_row_loss [rows], d_margin [pairs], d_logprob [rows]: fp32, each may be NULL.  row_loss and logprob of rows that
  *     do not count are 0.
  *   d_grad : NULL: none.  Else [rows][ld_grad] of grad_type: grad_scale * dloss/dz for every row and its live columns, zeros in rows
- *     that do not count.  It may be the logits' own memory if type and stride are the same, and must not overlap them else.
+ *     that do not count.  It may be the logits' own memory if type and stride are the same, and must not share their range of addresses else.
  *   d_workspace : device scratch of at least nanospec_loss_workspace(rows, V) bytes (-1: sizes out of range), 256-byte aligned.  Calls
  *     that may overlap must not share one.
- * Limits: rows * ld below 2^60, V <= 2^30.  Errors: EINVAL (null, sizes < 1, ld < V, an unknown type, d_ids without d_n or
+ * Limits: rows <= 2^22, rows * ld below 2^60, V <= 2^30; logits and gradients aligned to their type.  Errors: EINVAL (null, sizes < 1, ld < V, an unknown type, d_ids without d_n or
  * the other way round, clip_low or clip_high negative, kl_beta != 0 without d_ref, smoothing outside [0, 1], a NaN among these, bad
  * offsets), ECAPACITY (workspace too small, 2 pairs > NANOSPEC_MAX_BATCH), EHIP.  Asynchronous. */
 NANOSPEC_API int64_t nanospec_loss_workspace(int32_t rows, int32_t V);

@@ -116,22 +116,25 @@ nanospec_status vocab_call(nanospec_state* st, const int32_t* d_new, const int32
 
 bool aligned_to(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
+constexpr int32_t kMostHidden = 1 << 24, kMostLogitRows = 1 << 22;   // of a call: launches have less than 2^32 threads
+
 // sizes of an 8-bit product: 16-byte pieces, int32 sums of products up to 127 * 127, 32-bit byte offsets
 bool i8_sizes_ok(int64_t rows, int32_t d) { return rows >= 1 && d >= 16 && d % 16 == 0 && d <= 133136 && rows * d <= 0xffffffffll; }
 
 nanospec_status head_i8(const int8_t* W, const float* W_scale, const void* H, const int32_t* ids, const int32_t* n_dev, int32_t cap, int32_t V, int32_t batch, int32_t M,
                         int32_t d, int64_t ld, float* logits, void* ws, int64_t ws_bytes, void* stream) {
-  if (!aligned_to(W, 16) || !aligned_to(H, 16) || !aligned_to(ws, 256) || !i8_sizes_ok(V, d) || !i8_sizes_ok((int64_t)batch * M, d)) return NANOSPEC_EINVAL;
+  if (!aligned_to(W, 16) || !aligned_to(H, 16) || !aligned_to(ws, 256) || !i8_sizes_ok(V, d) || !i8_sizes_ok((int64_t)batch * M, d) || (int64_t)batch * M > kMostHidden) return NANOSPEC_EINVAL;
   if (ws_bytes < head_i8_workspace_bytes(batch * M, d)) return NANOSPEC_ECAPACITY;
+  if (ensure_device_configured() != hipSuccess) return NANOSPEC_EHIP;   // a flag test after the first call on the device
   return launch_head_i8(W, W_scale, H, ids, n_dev, cap, V, batch, M, d, ld, logits, static_cast<char*>(ws), static_cast<hipStream_t>(stream)) == hipSuccess ? NANOSPEC_OK
                                                                                                                                                    : NANOSPEC_EHIP;
 }
 
 // what a caller gave as rows of logits, for the kernels; without weights and with all rows counting
 nanospec_status logit_rows_of(const nanospec_logit_rows* in, const void* ws, int64_t ws_bytes, LogitRows* r) {
-  if (!in || !in->d_logits || !in->d_tokens || !ws || in->rows < 1 || in->V < 1 || in->V > (1 << 30) || in->ld < in->V || in->ld > (1ll << 60) / in->rows) return NANOSPEC_EINVAL;
+  if (!in || !in->d_logits || !in->d_tokens || !ws || in->rows < 1 || in->rows > kMostLogitRows || in->V < 1 || in->V > (1 << 30) || in->ld < in->V || in->ld > (1ll << 60) / in->rows) return NANOSPEC_EINVAL;
   if (in->type != NANOSPEC_F32 && in->type != NANOSPEC_BF16) return NANOSPEC_EINVAL;
-  if (!in->d_ids != !in->d_n || (in->d_ids && in->rows_per_list < 1) || !aligned_to(ws, 256)) return NANOSPEC_EINVAL;
+  if (!in->d_ids != !in->d_n || (in->d_ids && in->rows_per_list < 1) || !aligned_to(ws, 256) || !aligned_to(in->d_logits, in->type == NANOSPEC_F32 ? 4 : 2)) return NANOSPEC_EINVAL;
   if (ws_bytes < loss_workspace_bytes(in->rows, in->V)) return NANOSPEC_ECAPACITY;
   *r = LogitRows{in->d_logits, in->d_tokens, in->d_ids, in->d_n, nullptr, in->ld, in->type, in->rows, in->V, in->d_ids ? in->rows_per_list : in->rows, 0, in->rows};
   return NANOSPEC_OK;
@@ -140,7 +143,7 @@ nanospec_status logit_rows_of(const nanospec_logit_rows* in, const void* ws, int
 // the gradient may lie on the logits exactly, not across them
 bool grad_ok(const LogitRows& r, const void* grad, int32_t type, int64_t ld) {
   if (!grad) return true;
-  if ((type != NANOSPEC_F32 && type != NANOSPEC_BF16) || ld < r.V || ld > (1ll << 60) / r.rows) return false;
+  if ((type != NANOSPEC_F32 && type != NANOSPEC_BF16) || ld < r.V || ld > (1ll << 60) / r.rows || !aligned_to(grad, type == NANOSPEC_F32 ? 4 : 2)) return false;
   if (grad == r.z) return type == r.type && ld == r.ld;
   const uintptr_t z0 = reinterpret_cast<uintptr_t>(r.z), g0 = reinterpret_cast<uintptr_t>(grad);
   const uintptr_t z1 = z0 + ((uintptr_t)(r.rows - 1) * r.ld + r.V) * (r.type == NANOSPEC_F32 ? 4 : 2);
@@ -481,12 +484,11 @@ nanospec_status nanospec_quantize_rows(const void* d_X_bf16, int64_t rows, int32
   return launch_quantize_rows(d_X_bf16, rows, d, d_Q, d_scale, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? NANOSPEC_OK : NANOSPEC_EHIP;
 }
 
-int64_t nanospec_head_i8_workspace(int32_t rows, int32_t d) { return i8_sizes_ok(rows, d) ? head_i8_workspace_bytes(rows, d) : -1; }
+int64_t nanospec_head_i8_workspace(int32_t rows, int32_t d) { return i8_sizes_ok(rows, d) && rows <= kMostHidden ? head_i8_workspace_bytes(rows, d) : -1; }
 
 nanospec_status nanospec_dense_head_i8(const int8_t* d_W_i8, const float* d_W_scale, const void* d_H_bf16, int32_t V, int32_t d, int32_t M_total, float* d_logits,
                                        void* d_workspace, int64_t workspace_bytes, void* hip_stream) {
   if (!d_W_i8 || !d_W_scale || !d_H_bf16 || !d_logits || !d_workspace || M_total < 1) return NANOSPEC_EINVAL;
-  if (ensure_device_configured() != hipSuccess) return NANOSPEC_EHIP;   // a flag test after the first call on the device
   return head_i8(d_W_i8, d_W_scale, d_H_bf16, nullptr, nullptr, V, V, 1, M_total, d, V, d_logits, d_workspace, workspace_bytes, hip_stream);
 }
 
@@ -497,7 +499,7 @@ nanospec_status nanospec_sparse_head_i8(nanospec_state* st, const int8_t* d_W_i8
   return head_i8(d_W_i8, d_W_scale, d_H_bf16, st->vp.ids, st->vp.n, st->vp.cap, st->V, st->batch, M, st->d, st->vp.cap, d_logits, d_workspace, workspace_bytes, hip_stream);
 }
 
-int64_t nanospec_loss_workspace(int32_t rows, int32_t V) { return rows < 1 || V < 1 || V > (1 << 30) ? -1 : loss_workspace_bytes(rows, V); }
+int64_t nanospec_loss_workspace(int32_t rows, int32_t V) { return rows < 1 || rows > kMostLogitRows || V < 1 || V > (1 << 30) ? -1 : loss_workspace_bytes(rows, V); }
 
 nanospec_status nanospec_token_logprob(const nanospec_logit_rows* rows, float* d_logprob, void* d_workspace, int64_t workspace_bytes, void* hip_stream) {
   LogitRows r;

@@ -178,10 +178,23 @@ inline FewPlan few_plan(int32_t M, int32_t d, int32_t batch, int32_t cap_rows, b
 // 10.2, 2048 37 / 35; 1000, 128 12.2 / 12.6, 2048 17.2 / 20.0; 152064, of which 21000 columns are read twice, 2048 612 / 430.
 inline bool policy_fuses(int32_t rows, int32_t V) { return rows >= 128 && V >= 4096; }
 
-// The 8-bit head's block shapes beyond: as many bytes a step hold twice the columns.  256 x 256 blocks with the scales do not fit LDS, so d that is no multiple of 128 takes 256 x 128.
+// The 8-bit head's block shapes beyond: as many bytes a step hold twice the columns, so that a block's walk is half as many steps and larger blocks pay earlier than above.  By the work, rows (what the
+// lists have room for) times hidden rows in 64s; us on lists of n live rows of 4096, without the hidden rows' 3 us:
+//   up to 32 hidden rows: 32 x 32, from 8192 rows on 64 x 32 (n = 9000, M = 32 16.2 / 14.3, 3 sequences of 3000, M = 20 15.9 / 14.1, n = 3000 11.4 / 13.6);
+//   32 x 32 below 6144 (n = 3000, M = 64 11.6, 32 x 64 12.8; M = 100 14.6 / 13.2), 32 x 64 below 8800 (4 sequences of 2000, M = 60 18.3 / 14.0, 64 x 64 16.4; n = 9000, M = 64
+//   19.1 / 16.9), 64 x 64 below 24000 (n = 9000, M = 64 16.9, 128 x 64 22.6), 128 x 64 below 65536 (dense 8000, M = 256 24.2 / 23.0; n = 30000, M = 100 51 / 48, 256 x 128 52);
+//   more: up to 64 hidden rows or several sequences 128 x 64 on lists (64 of 2300, M = 60 117 for 64 x 64, 110), 64 x 64 dense (128256 rows, M = 64 134 / 142, M = 33 125 / 136);
+//   up to 128, or up to 140000, 256 x 128 (n = 30000, M = 200 52 / head_gemm 61, 128 x 64 68; dense 50000, M = 100 71 / 74 / 78); more: head_gemm_i8_kernel (dense 50000, M = 256 98 / 85,
+//   128256, M = 200 202 / 181) where d is a multiple of 128.  256 x 256 blocks with the scales do not fit LDS.
 inline WideShape i8_shape(int32_t M, int32_t d, int32_t batch, int32_t cap_rows, bool dense) {
-  const WideShape s = wide_shape(M, d / 2, batch, cap_rows, dense, d % 128 == 0);
-  return s == kWide256x256 ? kWide256x128 : s;
+  const int64_t rows = (int64_t)cap_rows * batch, work = rows * ((M + 63) / 64);
+  if (M <= 32) return rows < 8192 ? kWide32x32 : kWide64x32;
+  if (work < 6144) return kWide32x32;
+  if (work < 8800) return kWide32x64;
+  if (work < 24000) return kWide64x64;
+  if (work < 65536) return kWide128x64;
+  if (M <= 64 || batch > 1) return dense ? kWide64x64 : kWide128x64;
+  return M <= 128 || work < 140000 || d % 128 != 0 ? kWide256x128 : kWideGemm;
 }
 
 // Sequences hold many of the same rows, and a die's L2 sees a row again only if the sequences that hold it run there at the

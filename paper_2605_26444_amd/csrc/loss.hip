@@ -21,10 +21,17 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8_any __attribute__((ext_vector_type(8), aligned(2)));
 
 constexpr int kRowThreads = 256;         // of a workgroup that takes a piece of a row
-constexpr float kLog2e = 0x1.715476p+0f, kLog2eRest = 0x1.4ae0c0p-26f, kLn2 = 0.6931471805599453f;   // log2 e in two parts
+// log2 e lies between two fp32 numbers, 0.16 of their distance above the lower one.  With one of them for all exponents, every term of a row's sum is off by 1.3e-8 (or 7e-8) of
+// its exponent to the same side, which does not average out (1e-7 of the sum; seen in the margin of two answers, where most of the log-probabilities cancel).
+constexpr float kLog2e = 0x1.715476p+0f, kLog2eUp = 0x1.715478p+0f, kLog2eRest = 0x1.4ae0c0p-26f, kLn2 = 0.6931471805599453f;   // kLog2e + kLog2eRest: log2 e
 
-// x <= 0: off by 2^-24 (2 |x| + 2) of the result at most
-__device__ __forceinline__ float exp_neg(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+// x <= 0, between two maxima, for the sums: the exponent rounded once
+__device__ __forceinline__ float exp_neg(float x) {
+  x = fmaxf(x, -1000.f);                                   // exp is 0 from -104 on; -inf would meet itself below
+  const float y = x * kLog2e;
+  return __builtin_amdgcn_exp2f(y + fmaf(x, kLog2eRest, fmaf(x, kLog2e, -y)));
+}
+__device__ __forceinline__ float exp_neg_short(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }      // of a logit; NaN stays NaN
 
 template <typename T>
 struct Vec;
@@ -88,10 +95,8 @@ __device__ __forceinline__ Stat join(Stat a, Stat b) {
   return Stat{m, a.s * exp_neg(a.m - mm) + b.s * exp_neg(b.m - mm)};
 }
 
-// N more numbers.  exp(x - m) = 2^(L x - L m) with L = log2 e in two parts: rounded to one fp32, L would lower every exponent by 1.3e-8 of
-// itself, an error that does not average out over a row (1e-7 of the sum, seen in the margin of two answers, where most of
-// the log-probabilities cancels).  L x - c in two multiply-adds, as many instructions as x - m and a product; c = fl(L m), and what c is off
-// by multiplies the sum.
+// N more numbers: 2^(x l - c) with l one of the two neighbours of log2 e -- of sixteen numbers three take the upper one, which leaves the sum's bias a sixth --, c = fl(m l);
+// what c is off by multiplies the sum.  A multiply-add, the exponential and an addition a number.
 template <int N>
 __device__ __forceinline__ void take(Stat& t, const float (&x)[N]) {
   float top = x[0];
@@ -100,14 +105,18 @@ __device__ __forceinline__ void take(Stat& t, const float (&x)[N]) {
   const float m = fmaxf(t.m, top);
   float s = 0.f;
   if (fabsf(m) < 1e37f) {
-    const float c = m * kLog2e, off = fmaf(m, kLog2eRest, fmaf(m, kLog2e, -c));
+    const float c = m * kLog2e, cu = m * kLog2eUp;
+    float su = 0.f;
 #pragma unroll
-    for (int i = 0; i < N; ++i) s += __builtin_amdgcn_exp2f(fmaf(x[i], kLog2eRest, fmaf(x[i], kLog2e, -c)));
-    s = fmaf(s, -off * kLn2, s);
-  } else {                                                 // nothing but -inf so far, or L m does not fit
+    for (int i = 0; i < N; ++i) {
+      if (i % 6 == 3) su += __builtin_amdgcn_exp2f(fmaf(x[i], kLog2eUp, -cu));
+      else s += __builtin_amdgcn_exp2f(fmaf(x[i], kLog2e, -c));
+    }
+    s = fmaf(s, -kLn2 * fmaf(m, kLog2e, -c), s) + fmaf(su, -kLn2 * fmaf(m, kLog2eUp, -cu), su);
+  } else {                                                 // nothing but -inf so far, or m log2 e does not fit
     const float mm = finite_or_zero(m);
 #pragma unroll
-    for (int i = 0; i < N; ++i) s += exp_neg(x[i] - mm);
+    for (int i = 0; i < N; ++i) s += exp_neg_short(x[i] - mm);
   }
   t.s = t.s * exp_neg(t.m - finite_or_zero(m)) + s;
   t.m = m;
@@ -360,7 +369,7 @@ __global__ __launch_bounds__(1024) void policy_sum_kernel(int rows, const double
 // the caches.  Two launches over all rows instead read them twice from memory (2048 rows of 128256 in fp32: 1 GB).
 // A chunk is what the workgroup's threads hold in a piece each; a row's full chunks go to LDS first, then to registers, the others and the row's end are streamed.
 template <typename T, typename G, int RC, int LC>
-__global__ __launch_bounds__(512, 2) void policy_fused_kernel(const LogitRows r, const PolicyArgs a, double* __restrict__ term, G* __restrict__ grad, int64_t ld_grad) {
+__global__ __launch_bounds__(512, 2) void policy_fused_kernel(const LogitRows r, const PolicyArgs a, double* __restrict__ term, G* grad, int64_t ld_grad) {
   constexpr int N = Vec<T>::N, CH = 512 * N, U = 16 / N;                  // U pieces: 16 numbers, what a step of the sums takes
   static_assert(RC % U == 0 && LC % U == 0 && LC <= RC, "whole steps");
   typedef typename Vec<T>::Raw Raw;
@@ -465,7 +474,7 @@ __global__ __launch_bounds__(512, 2) void policy_fused_kernel(const LogitRows r,
   }
   __syncthreads();
   const RowCoef k = shared_k;
-  auto value = [&](float x) { return k.c == 0.f ? 0.f : k.scale * exp_neg(x - k.m); };
+  auto value = [&](float x) { return k.c == 0.f ? 0.f : k.scale * exp_neg_short(x - k.m); };
   G* gt = g + tid * N;
   auto put = [&](int c, const Raw& y) {
     float x[N];
@@ -589,7 +598,7 @@ __device__ __forceinline__ void grad_piece(const T* z, G* g, const RowCoef& k, i
     return;
   }
   auto one = [&](float x, int c) {
-    const float p = k.scale * exp_neg(x - k.m);
+    const float p = k.scale * exp_neg_short(x - k.m);
     return c == k.col ? p + k.c : p;
   };
   int c = c0;
@@ -686,8 +695,8 @@ __global__ __launch_bounds__(kRowThreads) void few_rows_grad_kernel(const LogitR
 static int whole_threads(int32_t rows, int32_t V) { return rows < 128 || V < 16384 ? 0 : V < 32768 ? 256 : 512; }
 
 static RowCut row_cut(int32_t rows, int32_t V) {
-  int64_t pieces = (2048 + rows - 1) / rows;
-  const int64_t most = (V + 4095) / 4096;
+  int64_t pieces = (2048 + (int64_t)rows - 1) / rows;
+  const int64_t most = ((int64_t)V + 4095) / 4096;
   if (pieces > most) pieces = most;
   const int64_t span = ((V + pieces - 1) / pieces + 4095) / 4096 * 4096;
   return RowCut{(int32_t)((V + span - 1) / span), (int32_t)(span < V ? span : V)};

@@ -6,14 +6,14 @@ namespace nanospec {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-// WPR wavefronts a row, which holds what they can of it -- 32 numbers a lane -- in registers and reads the rest again, from the caches.
+// WPR wavefronts (1 or 4) a row, which holds what they can of it -- 32 numbers a lane -- in registers and reads the rest again, from the caches.
 template <int WPR>
-__global__ __launch_bounds__(WPR < 4 ? 256 : 64 * WPR) void quantize_rows_kernel(const uint16_t* __restrict__ X, int64_t rows, int d, int8_t* __restrict__ q,
-                                                                               float* __restrict__ scale) {
-  constexpr int P = 4, RPB = WPR < 4 ? 4 / WPR : 1, STEP = 512 * WPR;
-  const int tid = threadIdx.x, at = WPR < 4 ? tid % (64 * WPR) : tid;
-  const int64_t row = (int64_t)blockIdx.x * RPB + (RPB > 1 ? tid / (64 * WPR) : 0);
-  if (row >= rows) return;                                 // whole rows of a workgroup only where wavefronts do not meet
+__global__ __launch_bounds__(256) void quantize_rows_kernel(const uint16_t* __restrict__ X, int64_t rows, int d, int8_t* __restrict__ q, float* __restrict__ scale) {
+  static_assert(WPR == 1 || WPR == 4, "a row's wavefronts meet in a barrier, or there is one");
+  constexpr int P = 4, STEP = 512 * WPR;
+  const int tid = threadIdx.x, at = tid % (64 * WPR);
+  const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x, row = WPR == 4 ? block : block * 4 + tid / 64;
+  if (row >= rows) return;
   const uint16_t* x = X + row * d;
   u32x4 v[P];
 #pragma unroll
@@ -57,15 +57,14 @@ __global__ __launch_bounds__(WPR < 4 ? 256 : 64 * WPR) void quantize_rows_kernel
   if (at == 0) scale[row] = k.scale;
 }
 
-// Many rows: as few wavefronts a row as hold it.  Few: as many as there are numbers for, since a row's time is what a wavefront's chain of loads and rounding takes.
+// One wavefront for rows that it holds, else four (us, 1 / 4 / 16 wavefronts: 8 x 4096 3.6 / 2.5 / 2.7, 1024 x 4096 5.5 / 4.3 / 6.4, 512 x 2048 2.6 / 2.7 / 3.6, 32000 x 512 13 / 27 / 104,
+// 128256 x 4096 301 / 259 / 550: 6.1 TB/s read and written, 16 x 8192 6.1 / 2.6 / 2.9).
 hipError_t launch_quantize_rows(const void* X, int64_t rows, int32_t d, int8_t* q, float* scale, hipStream_t s) {
   const uint16_t* x = static_cast<const uint16_t*>(X);
-  const int wpr = rows >= 2048 ? (d <= 2048 ? 1 : d <= 8192 ? 4 : 16) : (d <= 512 ? 1 : d <= 2048 ? 4 : 16);
-  const int64_t grid = wpr == 1 ? (rows + 3) / 4 : rows;
-  if (grid > 0x7fffffff) return hipErrorInvalidValue;
-  if (wpr == 1) quantize_rows_kernel<1><<<dim3((unsigned)grid), 256, 0, s>>>(x, rows, d, q, scale);
-  else if (wpr == 4) quantize_rows_kernel<4><<<dim3((unsigned)grid), 256, 0, s>>>(x, rows, d, q, scale);
-  else quantize_rows_kernel<16><<<dim3((unsigned)grid), 1024, 0, s>>>(x, rows, d, q, scale);
+  const int64_t blocks = d <= 2048 ? (rows + 3) / 4 : rows, line = blocks < (1 << 20) ? blocks : 1 << 20;      // a launch has less than 2^32 threads along x
+  const dim3 grid((unsigned)line, (unsigned)((blocks + line - 1) / line));
+  if (d <= 2048) quantize_rows_kernel<1><<<grid, 256, 0, s>>>(x, rows, d, q, scale);
+  else quantize_rows_kernel<4><<<grid, 256, 0, s>>>(x, rows, d, q, scale);
   return hipGetLastError();
 }
 

@@ -465,7 +465,7 @@ __device__ __forceinline__ void gemm_block(const P product, const uint16_t* __re
   };
 
   float* scales = reinterpret_cast<float*>(smem + 2 * kGemmStage);
-  if constexpr (P::kScaled) {                              // waited for by the first counted wait, which leaves the operands' fetches in flight
+  if constexpr (P::kScaled) {                              // a round trip in front of the fetches: they are counted, and a load among them would not be
     if (tid < 256) {
       int64_t row = j0 + tid < n ? j0 + tid : j0;
       if (ids) row = ids[row];
@@ -651,8 +651,6 @@ hipError_t launch_head_wide_i8(const int8_t* W, const float* W_scale, const int8
 #define NS_SHAPE(S) \
   case S: return run_wide_i8<kWideBlocks[S].WR, kWideBlocks[S].WH, kWideBlocks[S].FR, kWideBlocks[S].FH, kWideBlocks[S].BK, kWideBlocks[S].D>(product, Wp, Hp, ids, n_dev, cap_rows, V, batch, M, d / 2, ld, logits, by_die, s)
   switch (shape) {
-    NS_SHAPE(kWide32x16);
-    NS_SHAPE(kWide64x16);
     NS_SHAPE(kWide32x32);
     NS_SHAPE(kWide64x32);
     NS_SHAPE(kWide32x64);
@@ -677,9 +675,7 @@ static hipError_t configure_i8() {
 }
 
 static hipError_t configure_wide_i8() {
-  hipError_t e = configure_i8<kWide32x16>();
-  if (e == hipSuccess) e = configure_i8<kWide64x16>();
-  if (e == hipSuccess) e = configure_i8<kWide32x32>();
+  hipError_t e = configure_i8<kWide32x32>();
   if (e == hipSuccess) e = configure_i8<kWide64x32>();
   if (e == hipSuccess) e = configure_i8<kWide32x64>();
   if (e == hipSuccess) e = configure_i8<kWide64x64>();

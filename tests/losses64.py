@@ -70,7 +70,8 @@ def gradient(rows, widths, dlp, slack, scale=1.0, kind="float32"):
 
 
 def policy(rows, old, ref, adv, weight, lo, hi, beta):
-    """(loss, its bound, row losses, their bounds, dlp, slack of dlp); asserts that no ratio is nearer to a border than it may be off"""
+    """(loss, its bound, row losses, their bounds, dlp, slack of dlp).  A ratio nearer to a border than it may be off -- delta of itself -- may
+    fall on either side: the loss is continuous there, its derivative is -ratio A on one side and 0 on the other"""
     R = len(rows)
     row, bound, dlp, slack = np.zeros(R), np.zeros(R), np.zeros(R), np.zeros(R)
     total = terms = 0.0
@@ -81,12 +82,12 @@ def policy(rows, old, ref, adv, weight, lo, hi, beta):
                 continue
             w = 1.0 if weight is None else float(weight[r])
             a, ratio = float(adv[r]), np.exp(q["lp"] - float(old[r]))
-            for edge in (1 - lo, 1 + hi):
-                assert not abs(ratio - edge) <= 4 * q["delta"] * ratio or a == 0, (r, ratio)
             free, held = ratio * a, float(np.clip(ratio, 1 - lo, 1 + hi)) * a
             x = -min(free, held) if free == free else free
             c = -free if free <= held or free != free else 0.0
             off, coff = abs(free) * q["delta"], abs(c) * q["delta"]
+            if min(abs(ratio - (1 - lo)), abs(ratio - (1 + hi))) <= 1.01 * q["delta"] * ratio:
+                coff = 1.01 * abs(free)
             if beta != 0:
                 gap = float(ref[r]) - q["lp"]
                 e = np.exp(gap)

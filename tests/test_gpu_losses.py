@@ -115,6 +115,52 @@ def test_policy(rows, V, kind, grad_kind):
     assert (gg[rows] == 9.0).all()
 
 
+MANY = [(128, 4096), (129, 4097), (131, 4103), (128, 9001), (150, 17001), (130, 33000), (128, 66003), (129, 131072), (128, 140001), (300, 5000)]
+
+
+@pytest.mark.parametrize("kind,grad_kind,inplace", [("f32", "f32", False), ("f32", "f32", True), ("f32", "bf16", False), ("bf16", "bf16", False), ("bf16", "bf16", True), ("bf16", "f32", False)])
+@pytest.mark.parametrize("rows,V", MANY)
+def test_policy_on_many_long_rows(rows, V, kind, grad_kind, inplace):
+    """rows that one workgroup holds: its registers, its LDS, what it streams, and every kind of end"""
+    g, z, t = logits(rows + V, rows, V, kind)
+    t[3], t[4], t[5], t[6] = 0, V - 1, -1, V // 2
+    z[7, t[7]] = -np.inf
+    z[8] = -np.inf
+    z[9, V // 3:] = float(torch.finfo(KIND[kind]).min)
+    z[10, ::2] = -np.inf
+    t[10] = 1
+    lp = lp_of(L.rows64(z.double().numpy(), t))
+    lp = np.where(np.isfinite(lp) & (lp > -700), lp, -2.0)
+    old, ref, adv = [(lp + g.randn(rows) * s).astype(np.float32) for s in (0.25, 0.5)] + [g.randn(rows).astype(np.float32)]
+    w = weights(g, rows)
+    w[3:11] = 0.5
+    zd = z.cuda()
+    zd[1], old[1] = float("nan"), np.nan
+    want = L.rows64(z.double().numpy(), t, weight=w)
+    loss, lb, row, rb, dlp, slack = L.policy(want, old, ref, adv, w, 0.2, 0.28, 0.05)
+    grad = zd if inplace else torch.full((rows + 1, V), 9.0, dtype=KIND[grad_kind], device="cuda")
+    got = run_policy(zd, t, old, ref, adv, w, 0.05, grad, scale=2.0)
+    near(got["lp"][:rows], lp_of(want), lp_bound(want), "logprob")
+    near(got["row"][:rows], row, rb, "rows")
+    near(got["loss"][:1], [loss], [lb], "loss")
+    gg = grad.float().cpu().numpy()
+    for r, (x, b) in enumerate(L.gradient(want, [V] * rows, dlp, slack, 2.0, NAME[KIND[grad_kind]])):
+        near(gg[r], x, b, r)
+    assert inplace or (gg[rows] == 9.0).all()
+    out = torch.empty(rows, device="cuda")
+    ws, n = space(rows, V)
+    zd = z.cuda()
+    B.nanospec_token_logprob(B.logit_rows(zd, dev(t, torch.int32)), out, ws, n)
+    everything = L.rows64(z.double().numpy(), t)
+    near(out.cpu(), lp_of(everything), lp_bound(everything), "logprob")
+
+
+@pytest.mark.parametrize("rows,V,off", [(150, 17001, [1, 40, 90, 100, 149]), (260, 40000, [0, 100, 255]), (129, 5000, [0, 1, 2, 3, 129]), (128, 70001, [5, 60, 128])])
+@pytest.mark.parametrize("kind,grad_kind", [("f32", "f32"), ("bf16", "bf16")])
+def test_preference_on_many_long_rows(rows, V, off, kind, grad_kind):
+    test_preference(rows, V, off, kind, grad_kind, False)
+
+
 @pytest.mark.parametrize("V", [63, 1000, 32001])
 def test_policy_without_weights_reference_and_gradient(V):
     rows = 6
@@ -241,7 +287,7 @@ def test_a_far_margin_neither_overflows_nor_loses_the_gradient():
         near(grad[r].cpu(), x, b, r)
 
 
-@pytest.mark.parametrize("counts,M", [([5, 0, 64, 700], 3), ([1], 4), ([2300] * 5, 8), ([9000, 4096], 2)])
+@pytest.mark.parametrize("counts,M", [([5, 0, 64, 700], 3), ([1], 4), ([2300] * 5, 8), ([9000, 4096], 2), ([9000, 0, 1, 4100, 8192] * 5, 7)])
 def test_on_the_active_sets_of_a_state(counts, M):
     V, batch = 20011, len(counts)
     g = np.random.RandomState(M)
