@@ -329,9 +329,9 @@ NANOSPEC_API nanospec_status nanospec_sparse_head_i8(nanospec_state* st, const i
  *                   ld = V = capacity, rows = batch * M).
  *   d_tokens      : int32 [rows], global ids.
  *   d_ids, d_n    : NULL: column j is id j.  Else the active sets, as nanospec_vocab_view gives them: row r's columns are the
- *                   ids d_ids[(r / rows_per_list) * V + j] for j < d_n[r / rows_per_list], ascending (rows_per_list = M); the
- *                   distribution is renormalised over them, as in nanospec_topk_logprob_remap.  Columns behind are neither read nor
- *                   written.
+ *                   ids d_ids[(r / rows_per_list) * V + j] for j < d_n[r / rows_per_list], ascending (rows_per_list = M, a list and
+ *                   a count for every M rows); the distribution is renormalised over them, as in nanospec_topk_logprob_remap.
+ *                   Columns behind are neither read nor written.
  * A logit of -inf has probability 0.  A token has no probability if it has no column, if its logit is -inf, or if exp of its
  * log-probability is 0 in 64 bits (below -745); a NaN or +inf among the columns of a row makes the row's results NaN. */
 #define NANOSPEC_F32 0

@@ -329,14 +329,21 @@ def nanospec_sparse_head_i8(st, d_W, d_W_scale, d_H, M, d_logits, d_workspace, w
                                          _stream(stream)), "nanospec_sparse_head_i8")
 
 
+_type_codes = None
+
+
 def _type_and_stride(t):
     """(type code, row stride) of a [rows][columns] tensor whose columns lie side by side"""
-    name = str(t.dtype)
-    if name not in ("torch.float32", "torch.bfloat16"):
-        raise ValueError(f"logits and their gradients are float32 or bfloat16, not {name}")
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or not t.is_cuda:
+    global _type_codes
+    if _type_codes is None:
+        import torch
+        _type_codes = {torch.float32: F32, torch.bfloat16: BF16}
+    kind, shape, stride = _type_codes.get(t.dtype), t.shape, t.stride()
+    if kind is None:
+        raise ValueError(f"logits and their gradients are float32 or bfloat16, not {t.dtype}")
+    if len(shape) != 2 or (shape[1] > 1 and stride[1] != 1) or not t.is_cuda:
         raise ValueError("logits and their gradients are device tensors [rows][columns] with columns side by side")
-    return (F32 if name == "torch.float32" else BF16), (t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1]))
+    return kind, (stride[0] if shape[0] > 1 else max(stride[0], shape[1]))
 
 
 def logit_rows(d_logits, d_tokens, V=None, ids=None, n=None, rows_per_list=1) -> LogitRows:

@@ -164,7 +164,7 @@ __device__ __forceinline__ int token_column(const LogitRows& r, int row, int n) 
 __device__ __forceinline__ int row_columns(const LogitRows& r, int row) {
   if (!r.n) return r.V;
   const int n = r.n[row / r.per_list];
-  return n < r.V ? n : r.V;
+  return n < 0 ? 0 : n < r.V ? n : r.V;
 }
 
 __device__ __forceinline__ bool row_counts(const LogitRows& r, int row) {
@@ -661,18 +661,17 @@ __device__ __forceinline__ double few_rows_coef(const LogitRows& r, int pieces, 
   return pair_coef(r, a, row, pair_loss(a, (double)a.beta * s).slope, answer & 1);       // of thread 0 only
 }
 
-// Few rows: the coefficients by every workgroup for itself, from the pieces' sums, in the launch that writes the gradient, and the totals by one workgroup more: a
-// launch less.
+// The coefficients by every workgroup for itself, from the sums of the pass before, in the launch that writes the gradient, and the totals by one workgroup more, the first: a launch less.
 template <typename T, typename G, typename A>
-__global__ __launch_bounds__(kRowThreads) void few_rows_grad_kernel(const LogitRows r, int pieces, int span, const Stat* part, const Place* at, const A a, double* term, G* grad,
+__global__ __launch_bounds__(kRowThreads) void few_rows_grad_kernel(const LogitRows r, int pieces, int cut, int span, const Stat* part, const Place* at, const A a, double* term, G* grad,
                                                                     int64_t ld_grad) {
   __shared__ double red[kRowThreads / 64];
   __shared__ RowCoef shared_k;
-  if ((int)blockIdx.x == r.rows * pieces) {
+  if (blockIdx.x == 0) {
     few_rows_total(r, pieces, part, at, a, term);
     return;
   }
-  const int row = blockIdx.x / pieces, piece = blockIdx.x - row * pieces;
+  const int block = blockIdx.x - 1, up = block / cut, row = r.rows - 1 - up, piece = block - up * cut;
   const int n = row_columns(r, row), c0 = piece * span, c1 = c0 + span < n ? c0 + span : n;
   if (c0 >= c1) return;
   RowCoef k{0.f, 0.f, 0.f, -1};
@@ -763,14 +762,17 @@ static hipError_t run_grad(const LogitRows& r, const LossSpace& s, void* grad, i
   return hipGetLastError();
 }
 
-// few rows: see few_rows_grad_kernel; a thread for every row of a pair
-static bool few_rows(int32_t rows) { return rows <= 128; }
+// Whether few_rows_grad_kernel writes the gradient.  Pairs: a thread for every row of the longest one, and rows that the workgroup of the totals gets through while the others write
+// (us, three launches / two: 37 rows of 32000 in fp32 14.4 / 11.5, 300 of 32000 29.2 / 26.3, 600 of 128256 155 / 150, 1021 of 152064 in bf16 184 / 178, 1000 of 8000 28.6 / 28.3).
+static bool policy_few_rows(int32_t rows) { return rows <= 128; }
+static bool pair_few_rows(int32_t rows, int32_t V, int32_t longest) { return longest <= kRowThreads && (rows <= 256 || (rows <= 2048 && V >= 8000)); }
 
 template <typename A>
 static hipError_t run_few_rows(const LogitRows& r, const LossSpace& s, const A& a, void* grad, int32_t type, int64_t ld, hipStream_t stream) {
-  const RowCut cut = stats_cut(r.rows, r.V);
+  const RowCut cut = row_cut(r.rows, r.V);
   const unsigned grid = (unsigned)(r.rows * cut.pieces) + 1;
-#define NS_FEW(T, G) few_rows_grad_kernel<T, G, A><<<dim3(grid), kRowThreads, 0, stream>>>(r, cut.pieces, cut.span, s.part, s.at, a, s.term, static_cast<G*>(grad), ld)
+  const int pieces = stats_cut(r.rows, r.V).pieces;
+#define NS_FEW(T, G) few_rows_grad_kernel<T, G, A><<<dim3(grid), kRowThreads, 0, stream>>>(r, pieces, cut.pieces, cut.span, s.part, s.at, a, s.term, static_cast<G*>(grad), ld)
   if (r.type == NANOSPEC_F32) {
     if (type == NANOSPEC_F32) NS_FEW(float, float);
     else NS_FEW(float, uint16_t);
@@ -829,7 +831,7 @@ hipError_t launch_policy_loss(const LogitRows& r, const PolicyArgs& a, void* gra
   if (grad && policy_fuses(r.rows, r.V)) return launch_policy_fused(r, a, s.term, grad, grad_type, ld_grad, stream);
   hipError_t e = run_stats(r, s, nullptr, stream);
   if (e != hipSuccess) return e;
-  if (grad && few_rows(r.rows)) return run_few_rows(r, s, a, grad, grad_type, ld_grad, stream);
+  if (grad && policy_few_rows(r.rows)) return run_few_rows(r, s, a, grad, grad_type, ld_grad, stream);
   policy_rows_kernel<<<dim3(1), 1024, 0, stream>>>(r, stats_cut(r.rows, r.V).pieces, s.part, s.at, a, grad ? s.coef : nullptr);
   e = hipGetLastError();
   return e == hipSuccess && grad ? run_grad(r, s, grad, grad_type, ld_grad, stream) : e;
@@ -839,7 +841,9 @@ hipError_t launch_preference_loss(const LogitRows& r, const PairArgs& a, const O
   const LossSpace s = loss_space(ws, r.rows, r.V);
   hipError_t e = run_stats(r, s, nullptr, stream);
   if (e != hipSuccess) return e;
-  if (grad && few_rows(r.rows)) return run_few_rows(r, s, PairFew{a, off}, grad, grad_type, ld_grad, stream);
+  int most = 0;
+  for (int p = 0; p < a.pairs; ++p) most = off.v[2 * p + 2] - off.v[2 * p] > most ? off.v[2 * p + 2] - off.v[2 * p] : most;
+  if (grad && pair_few_rows(r.rows, r.V, most)) return run_few_rows(r, s, PairFew{a, off}, grad, grad_type, ld_grad, stream);
   pair_rows_kernel<<<dim3(1), 1024, 0, stream>>>(r, stats_cut(r.rows, r.V).pieces, s.part, s.at, a, off, s.term, grad ? s.coef : nullptr);
   e = hipGetLastError();
   return e == hipSuccess && grad ? run_grad(r, s, grad, grad_type, ld_grad, stream) : e;
