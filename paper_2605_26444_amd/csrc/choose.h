@@ -137,7 +137,7 @@ struct FewPlan {
 inline bool few_supported(int32_t M, int32_t d) { return M <= 16 && d <= (M <= 8 ? 16384 : 8192); }
 
 // Whether it rounds the hidden rows itself, in every workgroup, or takes them from a launch of their own (3 us): 3000 rows of 4096, M = 8 6.8 us against 8.9, M = 1 5.4 / 8.0;
-// M = 16 10.6 / 9.8; 8192 columns, whose second half a workgroup reads twice, M = 4 12.3 / 10.7, M = 8 13.9 / 11.2.
+// M = 16 10.6 / 9.8; 8192 columns, whose second half a workgroup would read twice, M = 4 12.3 / 10.7, M = 8 13.9 / 11.2.
 inline bool few_rounds(int32_t M, int32_t d) { return d <= 4096 && (int64_t)M * d <= 32768; }
 
 // Shapes, us on lists of n live rows or dense (n = V = 128256), with 8 | 4 wavefronts:

@@ -29,7 +29,7 @@ __global__ __launch_bounds__(512, 2) void head_few_i8_kernel(const int8_t* __res
                                                              const int8_t* __restrict__ Hq, const float* __restrict__ H_scale, const int32_t* __restrict__ ids,
                                                              const int32_t* __restrict__ n_dev, int cap, int V, int M, int d, int64_t ld,
                                                              float* __restrict__ logits, int log_np, int nk, int log_ng, int seg) {
-  constexpr int MH = 4 * MT, HP = 8;                                      // HP: pieces of 16 bytes of a hidden row that a lane holds at once
+  constexpr int MH = 4 * MT, HP = 8;                                      // HP: pieces of 16 bytes of a hidden row that a lane holds: all of 4096 numbers
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const int log_rows = 2 + log_ng, seg_rows = seg << log_rows, segp = seg_rows + 4;
   float* hscale = reinterpret_cast<float*>(smem);                         // [MH]
@@ -125,11 +125,6 @@ __global__ __launch_bounds__(512, 2) void head_few_i8_kernel(const int8_t* __res
       for (int i = 0; i < HP; ++i)                                        // a piece past the end is a copy of the row's first
 #pragma unroll
         for (int e = 0; e < 4; ++e) top = bf16_tops(top, hx[i][e]);
-      for (int c = (HP * 64 + lane) * 8; c < d; c += 512) {
-        const u32x4 v = *reinterpret_cast<const u32x4*>(Hb + (int64_t)m * d + c);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) top = bf16_tops(top, v[e]);
-      }
       const I8Row k = i8_row(wave_top(top));
       char* to = hq + m * hstride;
       auto put = [&](auto tiny) {
@@ -142,7 +137,6 @@ __global__ __launch_bounds__(512, 2) void head_few_i8_kernel(const int8_t* __res
           const int c = (i * 64 + lane) * 8;
           if (c < d) one(c, hx[i]);
         }
-        for (int c = (HP * 64 + lane) * 8; c < d; c += 512) one(c, *reinterpret_cast<const u32x4*>(Hb + (int64_t)m * d + c));
       };
       if (k.p == 1.f) put(Flag<false>());
       else put(Flag<true>());

@@ -107,6 +107,56 @@ def test_dense_logits_to_the_last_bit(V, d, M):
     assert (got[M] == 5.0).all()
 
 
+@pytest.mark.parametrize("V,d,M", [(260, 16384, 1), (260, 16384, 8), (260, 16384, 9), (99, 12304, 5), (99, 8208, 16), (5000, 2064, 12), (40000, 2048, 8), (20011, 4096, 16), (20011, 4080, 3),
+                                   (100, 16400, 4), (3001, 4224, 140), (9000, 4112, 700), (2500, 640, 1024)])
+def test_dense_logits_of_other_shapes_to_the_last_bit(V, d, M):
+    test_dense_logits_to_the_last_bit(V, d, M)
+
+
+@pytest.mark.parametrize("M", [2, 20, 200])
+def test_rows_beyond_the_second_gigabyte(M):
+    """V d just below 2^32 bytes: rows at both ends and around 2^31"""
+    V, d = 1048575, 4096
+    w = torch.zeros((V, d), dtype=torch.int8, device="cuda")
+    where = torch.tensor([0, 1, 2 ** 19 - 1, 2 ** 19, 2 ** 19 + 1, V - 300, V - 2, V - 1])
+    some = torch.from_numpy(synth.rand_int(9, 0, 0, len(where) * d, -127, 127).reshape(-1, d).astype(np.int8))
+    w[where.cuda()] = some.cuda()
+    scale = torch.ones(V, device="cuda")
+    h = rows_bf16(10, M, d)
+    out = torch.full((M, V), 5.0, device="cuda")
+    ws, n = workspace(M, d)
+    B.nanospec_dense_head_i8(w, scale, h.cuda(), V, d, M, out, ws, n)
+    qh, sh = quantized(h)
+    assert same(out[:, where.cuda()].cpu().numpy(), expected(some.numpy(), np.ones(len(where), np.float32), qh, sh))
+    out[:, where.cuda()] = 0
+    assert not out.any()
+
+
+def test_as_many_sequences_as_a_state_holds():
+    test_active_rows_to_the_last_bit([(7 * b) % 40 for b in range(256)], None, 2, 64)
+
+
+@pytest.mark.parametrize("M", [3, 40])
+def test_on_a_stream_of_the_callers(M):
+    """the inputs are written on the same stream just before, the results are read on it just after"""
+    V, d = 900, 512
+    w, h = rows_bf16(7, V, d, 0.02), rows_bf16(8, M, d)
+    qw, sw = quantized(w)
+    W, S, fresh = torch.from_numpy(qw).cuda(), torch.from_numpy(sw).cuda(), h.cuda()
+    H, out = torch.zeros((M, d), dtype=torch.bfloat16, device="cuda"), torch.zeros((M, V), device="cuda")
+    ws, n = workspace(M, d)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        busy = torch.zeros(1 << 28, device="cuda").add_(1).add_(1)
+        H.copy_(fresh)
+    B.nanospec_dense_head_i8(W, S, H, V, d, M, out, ws, n, stream=side)
+    with torch.cuda.stream(side):
+        copy = out.clone()
+    side.synchronize()
+    assert same(copy.cpu().numpy(), expected(qw, sw, *quantized(h))) and busy[0] == 2
+
+
 @pytest.mark.parametrize("M", [1, 8, 16, 17, 64, 200])
 def test_the_largest_sums_are_exact(M):
     V, d = 20, 133136

@@ -274,6 +274,67 @@ def test_preference(rows, V, off, kind, grad_kind, plain):
     assert (gg[rows] == 9.0).all()
 
 
+@pytest.mark.parametrize("rows,V,off", [(600, 9000, [0, 400, 590]), (300, 100, [0, 270, 300]), (258, 20000, [0, 257, 258]), (40, 5001, [1, 15, 33])])
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_preference_on_long_answers_and_in_place(rows, V, off, kind):
+    g, z, t = logits(rows + V, rows, V, kind)
+    inside = (np.arange(rows) >= off[0]) & (np.arange(rows) < off[-1])
+    w = weights(g, rows)
+    ref = (lp_of(L.rows64(z.double().numpy(), t)) + g.randn(rows) * 0.4).astype(np.float32)
+    zd = z.cuda()
+    got = run_preference(zd, t, off, ref, w, 0.02, 0.1, zd)
+    want = L.rows64(z.double().numpy(), t, weight=w, inside=inside)
+    loss, lb, margin, mb, dlp, slack = L.preference(want, off, ref, w, 0.02, 0.1)
+    near(got["margin"][:-1], margin, mb, "margin")
+    near(got["loss"][:1], [loss], [lb], "loss")
+    gg = zd.float().cpu().numpy()
+    for r, (x, b) in enumerate(L.gradient(want, [V] * rows, dlp, slack, 1.0, NAME[KIND[kind]])):
+        near(gg[r], x, b, r)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_more_logits_than_32_bits_count(kind):
+    rows, V = 17000, 128256
+    z = torch.zeros((rows, V), dtype=KIND[kind], device="cuda")
+    some = [0, 1, 8371, 8372, 16743, 16744, 16745, rows - 1]                # around 2^30 and 2^31 elements
+    g, zs, ts = logits(3, len(some), V, kind)
+    z[torch.tensor(some).cuda()] = zs.cuda()
+    t = np.full(rows, 7, np.int32)
+    t[some] = ts
+    lp = lp_of(L.rows64(zs.double().numpy(), ts))
+    old, ref, adv = (np.full(rows, -np.log(V), np.float32) for _ in range(3))
+    old[some], ref[some], adv[some] = lp + 0.1, lp - 0.2, g.randn(len(some))
+    got = run_policy(z, t, old, ref, adv, None, 0.05, z)
+    want = L.rows64(zs.double().numpy(), ts)
+    _, _, row, rb, dlp, slack = L.policy(want, old[some], ref[some], adv[some], None, 0.2, 0.28, 0.05)
+    near(got["lp"][some], lp_of(want), lp_bound(want), "logprob")
+    near(got["row"][some], row, rb, "rows")
+    for r, (x, b) in zip(some, L.gradient(want, [V] * len(some), dlp, slack, 1.0, NAME[KIND[kind]])):
+        near(z[r].float().cpu(), x, b, r)
+    flat = np.delete(got["lp"][:rows], some)
+    assert np.abs(flat + np.log(V)).max() < 1e-5
+
+
+def test_on_a_stream_of_the_callers():
+    rows, V = 60, 3001
+    g, z, t = logits(4, rows, V, "f32")
+    zd, td, fresh = torch.zeros((rows, V), device="cuda"), dev(t, torch.int32), z.cuda()
+    out = torch.zeros(rows, device="cuda")
+    ws, n = space(rows, V)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        busy = torch.zeros(1 << 28, device="cuda").add_(1).add_(1)
+        zd.copy_(fresh)
+    B.nanospec_token_logprob(B.logit_rows(zd, td), out, ws, n, stream=side)
+    with torch.cuda.stream(side):
+        copy = out.clone()
+    side.synchronize()
+    want = L.rows64(z.double().numpy(), t)
+    near(copy.cpu(), lp_of(want), lp_bound(want), "logprob")
+    assert busy[0] == 2
+
+
 def test_a_far_margin_neither_overflows_nor_loses_the_gradient():
     z = torch.tensor([[0.0, 300.0], [0.0, 0.0], [0.0, 0.0], [0.0, 300.0]])
     t = np.zeros(4, np.int32)
@@ -324,16 +385,17 @@ def test_on_the_active_sets_of_a_state(counts, M):
     st.close()
 
 
-def test_captured_and_replayed():
+@pytest.mark.parametrize("rows", [40, 200, 700])
+def test_captured_and_replayed(rows):
     """a training step's three calls in a graph, replayed against new inputs with eager work between"""
-    rows, V = 40, 9001
+    V = 9001
     g, z, t = logits(21, rows, V, "f32")
     old, ref, adv = policy_inputs(g, z, t, rows)
     w = weights(g, rows)
     zd, td, args = z.cuda(), dev(t, torch.int32), [dev(x) for x in (old, ref, adv, w)]
     outs = [{"loss": torch.zeros(1, device="cuda"), "grad": torch.zeros((rows, V), device="cuda"), "lp": torch.zeros(rows, device="cuda")} for _ in range(2)]
     spaces = [space(rows, V) for _ in range(2)]
-    off = [0, 9, 19, 28, 40]
+    off = [0, 9, 19, 28, rows]
 
     def both(o, s):
         src = B.logit_rows(zd, td)
