@@ -27,6 +27,7 @@
  *   - All functions return a nanospec_status; nothing aborts or throws.  Argument errors are
  *     found on the host before anything is launched, in which case nothing is enqueued.
  *   - A state object must not be used from two streams at once.
+ *   - Calls without a state run on the device that is current; every device buffer has to be that device's.
  *   - bf16 = upper 16 bits of an IEEE fp32.  Products are accumulated in fp32.
  */
 #ifndef NANOSPEC_H_

@@ -311,7 +311,23 @@ def nanospec_union_view(st):
     return tuple(x.value for x in ptrs) + (cap.value, share.value)
 
 
+_current_device = None
+
+
+def _here(where, *tensors):
+    """a call without a state launches on the current device: its tensors have to be that device's"""
+    global _current_device
+    if _current_device is None:
+        import torch
+        _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    device = _current_device()
+    for t in tensors:
+        if t is not None and not isinstance(t, int) and t.get_device() != device:
+            raise ValueError(f"{where}: a tensor of device {t.get_device()}, while device {device} is the current one")
+
+
 def nanospec_quantize_rows(d_X, rows, d, d_Q, d_scale, stream=None):
+    _here("nanospec_quantize_rows", d_X, d_Q)
     _check(lib().nanospec_quantize_rows(_ptr(d_X), rows, d, _ptr(d_Q), _ptr(d_scale), _stream(stream)), "nanospec_quantize_rows")
 
 
@@ -320,6 +336,7 @@ def nanospec_head_i8_workspace(rows, d) -> int:
 
 
 def nanospec_dense_head_i8(d_W, d_W_scale, d_H, V, d, M_total, d_logits, d_workspace, workspace_bytes, stream=None):
+    _here("nanospec_dense_head_i8", d_W, d_H, d_logits)
     _check(lib().nanospec_dense_head_i8(_ptr(d_W), _ptr(d_W_scale), _ptr(d_H), V, d, M_total, _ptr(d_logits), _ptr(d_workspace), workspace_bytes,
                                         _stream(stream)), "nanospec_dense_head_i8")
 
@@ -362,6 +379,7 @@ def nanospec_loss_workspace(rows, V) -> int:
 
 
 def nanospec_token_logprob(rows, d_logprob, d_workspace, workspace_bytes, stream=None):
+    _here("nanospec_token_logprob", rows.keep and rows.keep[0], d_logprob)
     _check(lib().nanospec_token_logprob(rows, _ptr(d_logprob), _ptr(d_workspace), workspace_bytes, _stream(stream)), "nanospec_token_logprob")
 
 
@@ -377,6 +395,7 @@ def _grad(rows, d_grad):
 
 def nanospec_policy_loss(rows, d_old, d_ref, d_adv, d_weight, clip_low, clip_high, kl_beta, d_loss, d_row_loss, d_logprob, d_grad, d_workspace,
                          workspace_bytes, grad_scale=1.0, stream=None):
+    _here("nanospec_policy_loss", rows.keep and rows.keep[0], d_loss, d_grad)
     g, kind, ld = _grad(rows, d_grad)
     _check(lib().nanospec_policy_loss(rows, _ptr(d_old), _ptr(d_ref), _ptr(d_adv), _ptr(d_weight), clip_low, clip_high, kl_beta, _ptr(d_loss),
                                       _ptr(d_row_loss), _ptr(d_logprob), g, kind, ld, grad_scale, _ptr(d_workspace), workspace_bytes,
@@ -389,6 +408,7 @@ def nanospec_preference_loss(rows, h_off, d_ref, d_weight, beta, smoothing, d_lo
     off, op = _off(h_off)
     if off.size % 2 == 0:
         raise ValueError("h_off has a number more than there are answers, which come in pairs")
+    _here("nanospec_preference_loss", rows.keep and rows.keep[0], d_loss, d_grad)
     g, kind, ld = _grad(rows, d_grad)
     _check(lib().nanospec_preference_loss(rows, op, off.size // 2, _ptr(d_ref), _ptr(d_weight), beta, smoothing, _ptr(d_loss), _ptr(d_margin),
                                           _ptr(d_logprob), g, kind, ld, grad_scale, _ptr(d_workspace), workspace_bytes,

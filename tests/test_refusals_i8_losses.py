@@ -128,3 +128,22 @@ def test_shape_of_the_few_row_head(M, d, batch, cap, want):
     (200, 4096, 1, 30016, False, "256x128"), (256, 4096, 1, 50000, True, "gemm"), (1024, 4096, 1, 128256, True, "gemm"), (1024, 4112, 1, 128256, True, "256x128")])
 def test_block_shape_of_the_8_bit_head(M, d, batch, cap, dense, want):
     assert choose.rows_by_hidden(choose_i8.i8_shape(M, d, batch, cap, dense)) == want
+
+
+class Elsewhere:
+    """stands for a tensor of another device"""
+
+    def get_device(self):
+        return 3
+
+
+def test_tensors_of_another_device(lib, monkeypatch):
+    monkeypatch.setattr(B, "_current_device", lambda: 0)
+    e = Elsewhere()
+    rows = source()
+    rows.keep = (e,)
+    for call in (lambda: B.nanospec_quantize_rows(e, 1, 16, P, P), lambda: B.nanospec_dense_head_i8(P, P, e, 64, 64, 1, P, P, 1 << 40),
+                 lambda: B.nanospec_token_logprob(rows, P, P, 1 << 40), lambda: B.nanospec_policy_loss(source(), P, P, P, None, 0.2, 0.2, 0.1, e, None, None, None, P, 1 << 40),
+                 lambda: B.nanospec_preference_loss(source(), [0, 1, 2], None, None, 0.1, 0.0, P, None, None, e, P, 1 << 40)):
+        with pytest.raises(ValueError, match="device 3"):
+            call()
