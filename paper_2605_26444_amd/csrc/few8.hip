@@ -4,6 +4,10 @@
 // A call on few rows is one launch: a launch of its own for the hidden rows would cost as much as it has to read (2.5 us; 3000
 // rows of 4096 bytes are 2 us at the rate of a large read).  Every workgroup rounds all hidden rows -- M d numbers, from its die's
 // L2, while its first rows of W are on their way -- into LDS and takes its operands from there.
+//
+// What bounds it: on short lists one round trip after the other -- arguments, row count with ids and hidden rows, W, sums, logits -- and the rounding (3000 x 4096 in a graph: M = 1
+// 5.3 us, M = 8 6.8, without any rounding 5.4); on the whole matrix HBM (128256 x 4096, M = 8 88 us, 6.0 TB/s); on batches the bytes beyond a die's L2 (64 sequences of 2300 x
+// 4096, M = 8 56 us, 287 MB for 193 MB of distinct rows).  The bf16 kernels: 7.4, 172 and 103 us.
 #include "common.h"
 
 namespace nanospec {

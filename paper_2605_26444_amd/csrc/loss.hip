@@ -7,9 +7,11 @@
 //               pair = -(1 - e) log sigma(margin) - e log sigma(-margin), L = mean over the pairs
 //   gradient    dL/dz_j = c ([j == a] - p_j) with c = dL/d(log p) of the row
 //
-// Everything but the two passes over the logits is a few numbers a row.  So: rows_stats_kernel reads each row once (running maximum and
-// sum, the row cut into pieces where rows are few), one workgroup turns the pieces into log-probabilities, losses and a coefficient
-// per row (in 64 bits, sums in a fixed order: the result is reproducible bit for bit), rows_grad_kernel reads the logits again and writes the gradient.
+// Everything but the passes over the logits is a few numbers a row, in 64 bits, added in a fixed order: the result is reproducible bit for bit.
+// The passes: rows_stats_kernel reads each row once for its maximum and sum, a gradient pass reads the logits again and writes the gradient.  Between them one
+// workgroup turns the sums into log-probabilities, losses and a coefficient per row (rows_grad_kernel), or every workgroup of the gradient pass does that for
+// its row, a launch less (few_rows_grad_kernel).  A policy's coefficient depends on its row alone: from 128 long rows on one workgroup keeps a row between the two
+// and reads it once (policy_fused_kernel).  All are bound by HBM where rows are many and by launches where they are few.
 #include "common.h"
 
 namespace nanospec {
@@ -171,6 +173,8 @@ __device__ __forceinline__ bool row_counts(const LogitRows& r, int row) {
   return row >= r.first && row < r.last && (!r.weight || r.weight[row] != 0.f);
 }
 
+// Bound by HBM: 509 rows of 128256 in fp32 46 us (5.7 TB/s), 1021 of 152064 in bf16 64 us (4.9; a number costs 8 of the 64 lane-cycles a compute unit has, the exponential
+// 2.5 of them), where the loads of the next step are on their way: left to itself the compiler waits for each load of a step before the next (49 and 82 us).
 // Piece `blockIdx.x % pieces` of row `blockIdx.x / pieces`: maximum and sum of its columns to part[], and the token's column and logit, from
 // the workgroup that has the row's first columns, to at[].  Rows that do not count are not read.
 template <typename T, int NT>
@@ -366,7 +370,8 @@ __global__ __launch_bounds__(1024) void policy_sum_kernel(int rows, const double
 
 // A row's policy loss and its gradient by one workgroup, which keeps the row on the compute unit between the two: RC pieces of 16 bytes a thread in
 // registers, LC in LDS, so that up to (RC + LC) 8 KB of a row are read from memory once; what is beyond is read a second time, from
-// the caches.  Two launches over all rows instead read them twice from memory (2048 rows of 128256 in fp32: 1 GB).
+// the caches.  Two launches over all rows instead read them twice from memory: 2048 rows of 128256, fp32 to bf16, 518 us apart, 322 so (4.9 TB/s read and written, as a
+// copy; 512 KB of a row fit the compute unit's 672 of registers and LDS); to fp32 621 / 421.  Eight wavefronts, not sixteen: 256 registers a lane instead of 128.
 // A chunk is what the workgroup's threads hold in a piece each; a row's full chunks go to LDS first, then to registers, the others and the row's end are streamed.
 template <typename T, typename G, int RC, int LC>
 __global__ __launch_bounds__(512, 2) void policy_fused_kernel(const LogitRows r, const PolicyArgs a, double* __restrict__ term, G* grad, int64_t ld_grad) {
@@ -661,6 +666,8 @@ __device__ __forceinline__ double few_rows_coef(const LogitRows& r, int pieces, 
   return pair_coef(r, a, row, pair_loss(a, (double)a.beta * s).slope, answer & 1);       // of thread 0 only
 }
 
+// Bound by HBM where rows are many (1021 of 152064 in bf16 93 us, logits and gradient at 6.7 TB/s, some of the logits from the caches), else by the coefficients' 64-bit functions: 37 rows of 32000 7.4
+// us, 7 rows of a policy 4.6.
 // The coefficients by every workgroup for itself, from the sums of the pass before, in the launch that writes the gradient, and the totals by one workgroup more, the first: a launch less.
 template <typename T, typename G, typename A>
 __global__ __launch_bounds__(kRowThreads) void few_rows_grad_kernel(const LogitRows r, int pieces, int cut, int span, const Stat* part, const Place* at, const A a, double* term, G* grad,
