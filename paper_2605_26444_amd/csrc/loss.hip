@@ -99,6 +99,10 @@ __device__ __forceinline__ Stat join(Stat a, Stat b) {
 
 // N more numbers: 2^(x l - c) with l one of the two neighbours of log2 e -- of sixteen numbers three take the upper one, which leaves the sum's bias a sixth --, c = fl(m l);
 // what c is off by multiplies the sum.  A multiply-add, the exponential and an addition a number.
+// That factor, 2^r with |r| at most half a step of c, is taken to first order, which is enough while r is small: below 2048 |c| < 2^12, |r| <= 2^-13, and what is dropped,
+// (r ln 2)^2 / 2, is within 2^-28.  It is not for a row of -1e9, whose r may be 64.  Beyond, the maximum is subtracted first: one rounding of the difference, a subtraction a number more.
+constexpr float kNearMax = 2048.f;
+
 template <int N>
 __device__ __forceinline__ void take(Stat& t, const float (&x)[N]) {
   float top = x[0];
@@ -106,7 +110,7 @@ __device__ __forceinline__ void take(Stat& t, const float (&x)[N]) {
   for (int i = 1; i < N; ++i) top = fmaxf(top, x[i]);
   const float m = fmaxf(t.m, top);
   float s = 0.f;
-  if (fabsf(m) < 1e37f) {
+  if (fabsf(m) < kNearMax) {
     const float c = m * kLog2e, cu = m * kLog2eUp;
     float su = 0.f;
 #pragma unroll
@@ -115,10 +119,10 @@ __device__ __forceinline__ void take(Stat& t, const float (&x)[N]) {
       else s += __builtin_amdgcn_exp2f(fmaf(x[i], kLog2e, -c));
     }
     s = fmaf(s, -kLn2 * fmaf(m, kLog2e, -c), s) + fmaf(su, -kLn2 * fmaf(m, kLog2eUp, -cu), su);
-  } else {                                                 // nothing but -inf so far, or m log2 e does not fit
+  } else {                                                 // far from zero, infinite, or nothing but -inf so far
     const float mm = finite_or_zero(m);
 #pragma unroll
-    for (int i = 0; i < N; ++i) s += exp_neg_short(x[i] - mm);
+    for (int i = 0; i < N; ++i) s += __builtin_amdgcn_exp2f((x[i] - mm) * (i % 6 == 3 ? kLog2eUp : kLog2e));
   }
   t.s = t.s * exp_neg(t.m - finite_or_zero(m)) + s;
   t.m = m;

@@ -1,0 +1,72 @@
+"""Losses on logits of every size and on rows at the edges of what they accept, against 64 bits; tolerances are those derived in losses64.py:
+a logit's distance from its row's maximum carries one rounding, whatever the maximum is."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import losses64 as L
+import test_gpu_losses as T
+from paper_2605_26444_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+
+def compare(z, t, old, ref, adv, grad_kind="f32"):
+    """log-probabilities, policy loss and preference loss of rows that all count, each with its gradient"""
+    rows, V = z.shape
+    zd, want = z.cuda(), L.rows64(z.double().numpy(), t)
+    out = torch.empty(rows, device="cuda")
+    ws, n = T.space(rows, V)
+    B.nanospec_token_logprob(B.logit_rows(zd, T.dev(t, torch.int32)), out, ws, n)
+    T.near(out.cpu(), T.lp_of(want), T.lp_bound(want), "logprob")
+    name = T.NAME[T.KIND[grad_kind]]
+    grad = torch.empty((rows, V), dtype=T.KIND[grad_kind], device="cuda")
+
+    def gradients(dlp, slack, what):
+        gg = grad.float().cpu().numpy()
+        for r, (x, b) in enumerate(L.gradient(want, [V] * rows, dlp, slack, 1.0, name)):
+            T.near(gg[r], x, b, (what, r))
+
+    got = T.run_policy(zd, t, old, ref, adv, None, 0.05, grad)
+    loss, lb, row, rb, dlp, slack = L.policy(want, old, ref, adv, None, 0.2, 0.28, 0.05)
+    T.near(got["lp"][:rows], T.lp_of(want), T.lp_bound(want), "policy logprob")
+    T.near(got["row"][:rows], row, rb, "rows")
+    T.near(got["loss"][:1], [loss], [lb], "policy")
+    gradients(dlp, slack, "policy gradient")
+    off = [0, rows // 2, rows]
+    got = T.run_preference(zd, t, off, ref, None, 0.1, 0.05, grad)
+    loss, lb, margin, mb, dlp, slack = L.preference(want, off, ref, None, 0.1, 0.05)
+    T.near(got["margin"][:1], margin, mb, "margin")
+    T.near(got["loss"][:1], [loss], [lb], "preference")
+    gradients(dlp, slack, "preference gradient")
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [2047.0, 2049.0, 1e4, 1e5, 1e6, 1e7, 1e8, 1e9, 1e10, 1e20, 1e30, 1.1e37, 3e38])
+@pytest.mark.parametrize("rows,V", [(10, 300), (10, 9001), (130, 9001), (130, 17001), (129, 33000)])
+def test_logits_of_any_size(rows, V, size, kind):
+    """spans and all but a few columns masked with finite values, rows masked whole, rows far from zero on either side: in one
+    piece, in pieces, whole by one workgroup, and where loss and gradient are one workgroup's"""
+    g, z, t = T.logits(rows + V, rows, V, kind)
+    z = z.double()
+    keep = z[:, [V // 5, V // 2, V - 1]]
+    for r in range(rows):
+        x, sign = z[r], -1.0 if r % 10 < 5 else 1.0
+        if r % 5 == 0:
+            x[V // 7: V // 3] = sign * size
+        elif r % 5 == 1:
+            x[:] = sign * size
+            x[[V // 5, V // 2, V - 1]] = keep[r]
+        elif r % 5 == 2:
+            x[:] = sign * size
+        elif r % 5 == 3:
+            x[::2] = sign * size
+        else:
+            x += sign * size
+    z = z.to(T.KIND[kind])
+    for r in range(rows):                                   # a token that the row makes likely
+        x = z[r].double().numpy()
+        t[r] = g.choice(np.flatnonzero(x >= x.max() - 10))
+    old, ref, adv = T.policy_inputs(g, z, t, rows)
+    compare(z, t, old, ref, adv, kind)
