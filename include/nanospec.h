@@ -333,8 +333,8 @@ NANOSPEC_API nanospec_status nanospec_sparse_head_i8(nanospec_state* st, const i
  *                   ids d_ids[(r / rows_per_list) * V + j] for j < d_n[r / rows_per_list], ascending (rows_per_list = M, a list and
  *                   a count for every M rows); the distribution is renormalised over them, as in nanospec_topk_logprob_remap.
  *                   Columns behind are neither read nor written.
- * A logit of -inf has probability 0.  A token has no probability if it has no column, if its logit is -inf, or if exp of its
- * log-probability is 0 in 64 bits (below -745); a NaN or +inf among the columns of a row makes the row's results NaN. */
+ * A logit of -inf has probability 0.  A token has no probability if it has no column or if its logit is -inf; a NaN or +inf among
+ * the columns of a row makes the row's results NaN. */
 #define NANOSPEC_F32 0
 #define NANOSPEC_BF16 1
 typedef struct nanospec_logit_rows {
@@ -359,10 +359,12 @@ typedef struct nanospec_logit_rows {
  *     ratio = exp(log p_r - d_old[r]), gap = d_ref[r] - log p_r, A = d_adv[r],
  *     row_loss[r] = -min(ratio A, clamp(ratio, 1 - clip_low, 1 + clip_high) A) + kl_beta (exp(gap) - gap - 1),
  *     loss = sum of w_r row_loss[r] over the rows that count (a mean over tokens or answers is a matter of the weights).
- *     d_ref may be NULL if kl_beta is 0.  A row whose token has no probability has row_loss 0 and no gradient.
+ *     d_ref may be NULL if kl_beta is 0.  A row whose token has no probability, or one that is 0 in 64 bits (a log-probability
+ *     below -745, of which ratio and KL term take the exponential), has row_loss 0 and no gradient.
  *   nanospec_preference_loss: the preference loss on `pairs` pairs of answers.  Answer q covers rows h_off[q] .. h_off[q+1), pair p
  *     is answer 2p, the chosen one, and 2p + 1, the rejected one; rows outside h_off[0] .. h_off[2 pairs) do not count;
- *     S_q = sum of w_r (log p_r - d_ref[r]) (d_ref NULL: 0; a row whose token has no probability adds nothing),
+ *     S_q = sum of w_r (log p_r - d_ref[r]) (d_ref NULL: 0; every finite log p_r counts, also that of a token masked with a finite
+ *     value; a row whose token has no probability adds nothing and has no gradient),
  *     margin[p] = beta (S_2p - S_2p+1), loss = mean over p of -(1 - smoothing) log sigma(margin) - smoothing log sigma(-margin).
  *     h_off: host int32 [2 pairs + 1], non-decreasing, within 0 .. rows, read before the call returns; 2 pairs <= NANOSPEC_MAX_BATCH.
  *   d_loss fp32 [1]; d_row_loss [rows], d_margin [pairs], d_logprob [rows]: fp32, each may be NULL.  row_loss and logprob of rows that

@@ -268,7 +268,7 @@ struct RowResult {
   Stat t;
   double lp;
   int col;
-  bool has;          // the token has a probability: exp(lp) is not zero in 64 bits
+  bool has;          // the token has a probability: lp is not -inf
 };
 
 __device__ __forceinline__ RowResult finish_row(int row, int pieces, const Stat* __restrict__ part, const Place* __restrict__ at) {
@@ -278,7 +278,7 @@ __device__ __forceinline__ RowResult finish_row(int row, int pieces, const Stat*
   for (int i = 1; i < pieces; ++i) q.t = join(q.t, part[(int64_t)row * pieces + i]);
   q.lp = log_probability(a, q.t);
   q.col = a.col;
-  q.has = !(q.lp < -745.0);
+  q.has = !(q.lp == -INFINITY);
   return q;
 }
 
@@ -309,6 +309,10 @@ struct RowCoef {
 __device__ __forceinline__ RowCoef coef_of(const Stat& t, int col, double c, float grad_scale) {
   return RowCoef{t.m, (float)(-(c * grad_scale) / (double)t.s), (float)(c * grad_scale), col};
 }
+
+// A policy's ratio and KL term take exp of the log-probability: a row where that is 0 in 64 bits has no loss and no gradient.  A margin is a sum of log-probabilities, to which
+// every finite one counts.
+__device__ __forceinline__ bool policy_has(double lp) { return !(lp < -745.0); }
 
 // a row's policy loss and its derivative by the log-probability
 struct PolicyRow {
@@ -342,7 +346,7 @@ __device__ void policy_rows(const LogitRows& r, int pieces, const Stat* __restri
     if (row_counts(r, row)) {
       const RowResult q = finish_row(row, pieces, part, at);
       lp_out = (float)q.lp;
-      if (q.has) {
+      if (policy_has(q.lp)) {
         const PolicyRow x = policy_row(a, row, q.lp);
         const double w = weight_of(r, row);
         loss_out = (float)x.loss;
@@ -468,7 +472,7 @@ __global__ __launch_bounds__(512, 2) void policy_fused_kernel(const LogitRows r,
     const double lp = log_probability(pl, t);
     RowCoef k{0.f, 0.f, 0.f, -1};
     double loss = 0, sum = 0;
-    if (!(lp < -745.0)) {
+    if (policy_has(lp)) {
       const PolicyRow x = policy_row(a, row, lp);
       const double wt = weight_of(r, row);
       loss = x.loss;
@@ -649,7 +653,7 @@ __device__ __forceinline__ void few_rows_total(const LogitRows& r, int pieces, c
 }
 
 __device__ __forceinline__ double few_rows_coef(const LogitRows& r, int, const Stat*, const Place*, const PolicyArgs& a, int row, const RowResult& q, double*) {
-  return weight_of(r, row) * policy_row(a, row, q.lp).c;
+  return policy_has(q.lp) ? weight_of(r, row) * policy_row(a, row, q.lp).c : 0.0;
 }
 
 struct PairFew : PairArgs {

@@ -70,3 +70,34 @@ def test_logits_of_any_size(rows, V, size, kind):
         t[r] = g.choice(np.flatnonzero(x >= x.max() - 10))
     old, ref, adv = T.policy_inputs(g, z, t, rows)
     compare(z, t, old, ref, adv, kind)
+
+
+FAR = [-745.5, -746.0, -800.0, -1e4, -1e9, -1e30, float(torch.finfo(torch.float32).min)]
+
+
+@pytest.mark.parametrize("rows,V", [(14, 65), (14, 9001), (140, 33000), (602, 65), (602, 9001)])
+def test_preference_counts_every_finite_log_probability(rows, V):
+    """tokens whose probability is 0 in 64 bits, but not its logarithm, of which the margin is a sum; pairs of up to 256 rows and longer ones"""
+    g, z, t = T.logits(rows, rows, V, "f32")
+    off, where = ([0, 2, 4, 5, 8, 11, rows - 2] if rows < 150 else [0, rows // 2, rows - 2]), [1, 3, 4, 5, 8, 10, rows - 1]
+    for r, far in zip(where, FAR):                          # the last one lies behind the answers
+        z[r, t[r]] = far
+    inside = np.arange(rows) < off[-1]
+    want = L.rows64(z.double().numpy(), t, inside=inside)
+    for q in want:
+        if q is not None:
+            assert q["lp"] > -np.inf
+            q["has"] = True
+    assert sum(q is not None and q["lp"] < -745 for q in want) >= 6
+    lp = T.lp_of(want)
+    ref = np.where(lp < -1e6, -3.0, lp + g.randn(rows)).astype(np.float32)
+    for beta in (1e-3, 1e-30):
+        grad = torch.full((rows, V), 9.0, device="cuda")
+        got = T.run_preference(z.cuda(), t, off, ref, None, beta, 0.1, grad)
+        loss, lb, margin, mb, dlp, slack = L.preference(want, off, ref, None, beta, 0.1)
+        T.near(got["lp"][:rows], lp, T.lp_bound(want), "logprob")
+        T.near(got["margin"][:-1], margin, mb, "margin")
+        T.near(got["loss"][:1], [loss], [lb], "loss")
+        gg = grad.cpu().numpy()
+        for r, (x, b) in enumerate(L.gradient(want, [V] * rows, dlp, slack)):
+            T.near(gg[r], x, b, r)
