@@ -333,8 +333,8 @@ NANOSPEC_API nanospec_status nanospec_sparse_head_i8(nanospec_state* st, const i
  *                   ids d_ids[(r / rows_per_list) * V + j] for j < d_n[r / rows_per_list], ascending (rows_per_list = M, a list and
  *                   a count for every M rows); the distribution is renormalised over them, as in nanospec_topk_logprob_remap.
  *                   Columns behind are neither read nor written.
- * A logit of -inf has probability 0.  A token has no probability if it has no column or if its logit is -inf; a NaN or +inf among
- * the columns of a row makes the row's results NaN. */
+ * A logit of -inf has probability 0.  A token has no probability if it has no column (padding: whatever the row's columns hold) or if
+ * its logit is -inf.  Where the token has a column, a NaN or +inf among the row's columns makes the row's results NaN. */
 #define NANOSPEC_F32 0
 #define NANOSPEC_BF16 1
 typedef struct nanospec_logit_rows {

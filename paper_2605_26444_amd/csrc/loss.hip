@@ -140,9 +140,10 @@ struct Place {
   int col;
 };
 
-// -inf where the token has no column or its logit is -inf; both maximum and logit are exact, so only the sum carries a rounding
+// -inf where the token has no column, or its logit is -inf and the row's sum a number; both maximum and logit are exact, so only the sum carries a rounding
 __device__ __forceinline__ double log_probability(const Place& a, const Stat& t) {
-  return a.z == -INFINITY ? -INFINITY : ((double)a.z - (double)t.m) - log((double)t.s);
+  if (a.z == -INFINITY) return a.col >= 0 && t.s != t.s ? (double)t.s : -INFINITY;
+  return ((double)a.z - (double)t.m) - log((double)t.s);
 }
 
 // column of a row's token: the token itself, or its place in the ascending list; -1 if it has none.  One wavefront, every lane gets it.

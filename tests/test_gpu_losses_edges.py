@@ -101,3 +101,37 @@ def test_preference_counts_every_finite_log_probability(rows, V):
         gg = grad.cpu().numpy()
         for r, (x, b) in enumerate(L.gradient(want, [V] * rows, dlp, slack)):
             T.near(gg[r], x, b, r)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("rows,V", [(8, 50), (8, 9001), (130, 9001), (130, 17001)])
+def test_a_row_that_is_not_a_distribution_hides_behind_no_masked_token(rows, V, bad):
+    """row 1: the token's own logit is -inf beside a NaN or +inf, the row's results are NaN; row 2: a token without a column, the row adds nothing, whatever it
+    holds; row 4: -inf beside numbers"""
+    g, z, t = T.logits(rows, rows, V, "f32")
+    z[1, t[1]] = z[4, t[4]] = -np.inf
+    z[1, (t[1] + 1) % V] = z[2, 3] = bad
+    t[2] = V if rows < 100 else -1
+    zd, out = z.cuda(), torch.empty(rows, device="cuda")
+    ws, n = T.space(rows, V)
+    B.nanospec_token_logprob(B.logit_rows(zd, T.dev(t, torch.int32)), out, ws, n)
+    fine = np.ones(rows, bool)
+    fine[[1, 2, 4]] = False
+
+    def check(lp):
+        assert np.isnan(lp[1]) and np.isneginf(lp[[2, 4]]).all() and np.isfinite(lp[fine]).all()
+
+    check(out.cpu().numpy())
+    one, grad = np.ones(rows, np.float32), torch.full((rows, V), 9.0, device="cuda")
+    got = T.run_policy(zd, t, -one, -one, one, None, 0.05, grad)
+    check(got["lp"][:rows])
+    assert np.isnan(got["row"][1]) and (got["row"][[2, 4]] == 0).all() and np.isnan(got["loss"][0])
+    assert torch.isnan(grad[1]).any() and (grad[[2, 4]] == 0).all() and torch.isfinite(grad[torch.from_numpy(fine).cuda()]).all()
+    got = T.run_preference(zd, t, [0, 1, 2, 4, 7], None, None, 0.1, 0.0, grad)
+    check(np.where(np.arange(rows) < 7, got["lp"][:rows], out.cpu().numpy()))
+    assert np.isnan(got["margin"][0]) and np.isfinite(got["margin"][1]) and np.isnan(got["loss"][0])
+    assert torch.isnan(grad[:2]).any() and torch.isfinite(grad[2:]).all()
+    w = one.copy()
+    w[1] = 0                                                # and without that row everything is a number
+    got = T.run_policy(zd, t, -one, -one, one, w, 0.05, grad)
+    assert np.isfinite(got["loss"][0]) and torch.isfinite(grad).all()
