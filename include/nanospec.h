@@ -365,7 +365,8 @@ typedef struct nanospec_logit_rows {
  *     is answer 2p, the chosen one, and 2p + 1, the rejected one; rows outside h_off[0] .. h_off[2 pairs) do not count;
  *     S_q = sum of w_r (log p_r - d_ref[r]) (d_ref NULL: 0; every finite log p_r counts, also that of a token masked with a finite
  *     value; a row whose token has no probability adds nothing and has no gradient),
- *     margin[p] = beta (S_2p - S_2p+1), loss = mean over p of -(1 - smoothing) log sigma(margin) - smoothing log sigma(-margin).
+ *     margin[p] = beta (S_2p - S_2p+1), loss = mean over p of -(1 - smoothing) log sigma(margin) - smoothing log sigma(-margin),
+ *     a term without its factor being 0.  d_ref may be -inf (no probability under the reference): the margin is infinite then.
  *     h_off: host int32 [2 pairs + 1], non-decreasing, within 0 .. rows, read before the call returns; 2 pairs <= NANOSPEC_MAX_BATCH.
  *   d_loss fp32 [1]; d_row_loss [rows], d_margin [pairs], d_logprob [rows]: fp32, each may be NULL.  row_loss and logprob of rows that
  *     do not count are 0.

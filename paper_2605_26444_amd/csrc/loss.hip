@@ -520,7 +520,9 @@ struct PairLoss {
 __device__ __forceinline__ PairLoss pair_loss(const PairArgs& a, double margin) {
   const double e = (double)a.smoothing, less = log1p(exp(-fabs(margin)));               // log(1 + exp(-m)) = max(-m, 0) + less
   const double up = 1.0 / (1.0 + exp(margin)), down = 1.0 / (1.0 + exp(-margin));       // sigma(-m), sigma(m)
-  PairLoss p{(1.0 - e) * (fmax(-margin, 0.0) + less) + e * (fmax(margin, 0.0) + less), (1.0 - e) * -up + e * down};
+  // a margin is infinite where a reference gives a token no probability: a term whose factor is 0 adds nothing then, not 0 * inf
+  const double good = e == 1.0 ? 0.0 : (1.0 - e) * (fmax(-margin, 0.0) + less), bad = e == 0.0 ? 0.0 : e * (fmax(margin, 0.0) + less);
+  PairLoss p{good + bad, (1.0 - e) * -up + e * down};
   if (margin != margin) p.loss = margin;
   return p;
 }

@@ -135,3 +135,33 @@ def test_a_row_that_is_not_a_distribution_hides_behind_no_masked_token(rows, V, 
     w[1] = 0                                                # and without that row everything is a number
     got = T.run_policy(zd, t, -one, -one, one, w, 0.05, grad)
     assert np.isfinite(got["loss"][0]) and torch.isfinite(grad).all()
+
+
+@pytest.mark.parametrize("rows,V", [(6, 70), (6, 9001), (600, 70)])
+@pytest.mark.parametrize("smoothing,sign", [(0.0, 1), (1.0, -1), (0.0, -1), (1.0, 1), (0.25, 1), (0.25, -1)])
+def test_a_margin_without_end(rows, V, smoothing, sign):
+    """a reference that gives a token no probability (-inf, as nanospec_token_logprob says it) in one answer of the first pair: the margin is infinite, and the term
+    of the loss whose factor is 0 or whose logarithm is that of 1 adds nothing"""
+    g, z, t = T.logits(rows, rows, V, "f32")
+    off = [0, rows // 2 - 1, rows // 2, rows // 2 + 1, rows]
+    ref = np.full(rows, -2.0, np.float32)
+    ref[0 if sign > 0 else rows // 2 - 1] = -np.inf
+    grad = torch.full((rows, V), 9.0, device="cuda")
+    got = T.run_preference(z.cuda(), t, off, ref, None, 0.1, smoothing, grad)
+    assert got["margin"][0] == sign * np.inf
+    want = L.rows64(z.double().numpy(), t)
+    one, ob, margin, mb, dlp, slack = L.preference(want, off, np.where(np.isinf(ref), -2.0, ref), None, 0.1, smoothing)
+    T.near(got["margin"][1:2], margin[1:], mb[1:], "margin")
+    wrong = smoothing if sign > 0 else 1 - smoothing        # the factor of log sigma(-inf)
+    if wrong:
+        assert got["loss"][0] == np.inf
+    else:                                                   # half of the second pair's loss
+        second = ((1 - smoothing) * np.logaddexp(0, -margin[1]) + smoothing * np.logaddexp(0, margin[1])) / 2
+        T.near(got["loss"][:1], [second], [ob], "loss")
+    half = np.arange(rows) < rows // 2
+    slope = smoothing if sign > 0 else smoothing - 1
+    dlp[half] = np.where(np.arange(rows) < rows // 2 - 1, 1, -1)[half] * float(np.float32(0.1)) / 2 * slope
+    slack[half] = 1e-14
+    gg = grad.cpu().numpy()
+    for r, (x, b) in enumerate(L.gradient(want, [V] * rows, dlp, slack)):
+        T.near(gg[r], x, b, r)
