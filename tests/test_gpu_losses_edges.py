@@ -165,3 +165,29 @@ def test_a_margin_without_end(rows, V, smoothing, sign):
     gg = grad.cpu().numpy()
     for r, (x, b) in enumerate(L.gradient(want, [V] * rows, dlp, slack)):
         T.near(gg[r], x, b, r)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,V,off", [(2, 7, [0, 1, 2]), (20, 1000, [2, 9, 9, 13, 17]), (40, 9001, [3, 20, 37]), (600, 300, [0, 400, 590]), (150, 17001, [1, 40, 90, 100, 149]),
+                                        (130, 33000, [0, 60, 130]), (1300, 33, list(range(0, 1285, 5)))])
+def test_preference_without_a_gradient(rows, V, off, kind):
+    """the loss, the margins and the log-probabilities alone, as for a validation set; log-probabilities are the same to the last bit as beside a gradient"""
+    g, z, t = T.logits(rows + 3 * V, rows, V, kind)
+    inside = (np.arange(rows) >= off[0]) & (np.arange(rows) < off[-1])
+    zd = z.cuda()
+    zd[torch.from_numpy(~inside).cuda()] = float("nan")
+    for plain in (True, False):
+        w = None if plain else T.weights(g, rows)
+        ref = None if plain else (T.lp_of(L.rows64(z.double().numpy(), t)) + g.randn(rows) * 0.4).astype(np.float32)
+        want = L.rows64(z.double().numpy(), t, weight=w, inside=inside)
+        loss, lb, margin, mb, _, _ = L.preference(want, off, ref, w, 0.2, 0.1)
+        got = T.run_preference(zd, t, off, ref, w, 0.2, 0.1, None)
+        T.near(got["lp"][:rows], T.lp_of(want), T.lp_bound(want), "logprob")
+        T.near(got["margin"][:-1], margin, mb, "margin")
+        T.near(got["loss"][:1], [loss], [lb], "loss")
+        assert got["loss"][1] == got["margin"][-1] == got["lp"][rows] == 9.0
+        beside = T.run_preference(zd, t, off, ref, w, 0.2, 0.1, torch.empty((rows, V), device="cuda"))
+        assert np.array_equal(got["lp"], beside["lp"])
+        # margins and losses are added by workgroups of another size there
+        T.near(beside["margin"][:-1], margin, mb, "margin")
+        T.near(beside["loss"][:1], [loss], [lb], "loss")
