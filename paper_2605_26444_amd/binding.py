@@ -314,21 +314,30 @@ def nanospec_union_view(st):
 _current_device = None
 
 
-def _here(where, *tensors):
-    """a call without a state launches on the current device: its tensors have to be that device's"""
+def _device() -> int:
+    """the device that is current: a call without a state launches there"""
     global _current_device
     if _current_device is None:
         import torch
         _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
-    device = _current_device()
-    for t in tensors:
-        if t is not None and not isinstance(t, int) and t.get_device() != device:
-            raise ValueError(f"{where}: a tensor of device {t.get_device()}, while device {device} is the current one")
+    return _current_device()
+
+
+def _refuse(where, device, t):
+    if t.get_device() != device:
+        raise ValueError(f"{where}: a tensor of device {t.get_device()}, while device {device} is the current one")
+    raise AssertionError("device tensors must be contiguous CUDA/HIP tensors")
+
+
+def _here(where, device, *tensors):
+    """addresses of a call's contiguous tensors (None and ints pass), each of which has to be the current device's.  One line without further calls: a
+    small call is marshalling for the most part"""
+    return [t if t is None or isinstance(t, int) else t.data_ptr() if t.get_device() == device and t.is_contiguous() else _refuse(where, device, t) for t in tensors]
 
 
 def nanospec_quantize_rows(d_X, rows, d, d_Q, d_scale, stream=None):
-    _here("nanospec_quantize_rows", d_X, d_Q)
-    _check(lib().nanospec_quantize_rows(_ptr(d_X), rows, d, _ptr(d_Q), _ptr(d_scale), _stream(stream)), "nanospec_quantize_rows")
+    x, q, scale = _here("nanospec_quantize_rows", _device(), d_X, d_Q, d_scale)
+    _check(lib().nanospec_quantize_rows(x, rows, d, q, scale, _stream(stream)), "nanospec_quantize_rows")
 
 
 def nanospec_head_i8_workspace(rows, d) -> int:
@@ -336,9 +345,8 @@ def nanospec_head_i8_workspace(rows, d) -> int:
 
 
 def nanospec_dense_head_i8(d_W, d_W_scale, d_H, V, d, M_total, d_logits, d_workspace, workspace_bytes, stream=None):
-    _here("nanospec_dense_head_i8", d_W, d_H, d_logits)
-    _check(lib().nanospec_dense_head_i8(_ptr(d_W), _ptr(d_W_scale), _ptr(d_H), V, d, M_total, _ptr(d_logits), _ptr(d_workspace), workspace_bytes,
-                                        _stream(stream)), "nanospec_dense_head_i8")
+    w, scale, h, logits, ws = _here("nanospec_dense_head_i8", _device(), d_W, d_W_scale, d_H, d_logits, d_workspace)
+    _check(lib().nanospec_dense_head_i8(w, scale, h, V, d, M_total, logits, ws, workspace_bytes, _stream(stream)), "nanospec_dense_head_i8")
 
 
 def nanospec_sparse_head_i8(st, d_W, d_W_scale, d_H, M, d_logits, d_workspace, workspace_bytes, stream=None):
@@ -364,11 +372,15 @@ def _type_and_stride(t):
 
 
 def logit_rows(d_logits, d_tokens, V=None, ids=None, n=None, rows_per_list=1) -> LogitRows:
-    """nanospec_logit_rows of a [rows][columns] tensor (rows may be strided) and its tokens.  ids, n: the active sets, as
+    """nanospec_logit_rows of a [rows][columns] tensor (rows may be strided) and its tokens, all of one device.  ids, n: the active sets, as
     nanospec_vocab_view gives them; V: columns, all of the tensor's if not given."""
     kind, ld = _type_and_stride(d_logits)
     if d_tokens.numel() < d_logits.shape[0] or str(d_tokens.dtype) != "torch.int32":
         raise ValueError("a token (int32) for every row of logits is needed")
+    device = d_logits.get_device()
+    for t in (d_tokens, ids, n):
+        if t is not None and not isinstance(t, int) and t.get_device() != device:
+            raise ValueError(f"logits of device {device} with a tensor of device {t.get_device()}")
     r = LogitRows(d_logits.data_ptr(), _ptr(d_tokens), _ptr(ids), _ptr(n), ld, kind, d_logits.shape[0], d_logits.shape[1] if V is None else V, rows_per_list)
     r.keep = (d_logits, d_tokens, ids, n)
     return r
@@ -378,15 +390,24 @@ def nanospec_loss_workspace(rows, V) -> int:
     return int(lib().nanospec_loss_workspace(rows, V))
 
 
+def _rows_here(where, device, rows, *tensors):
+    """addresses as _here; the rows' tensors, which logit_rows found on one device, have to be the current device's too"""
+    if rows.keep and rows.keep[0].get_device() != device:
+        _refuse(where, device, rows.keep[0])
+    return _here(where, device, *tensors)
+
+
 def nanospec_token_logprob(rows, d_logprob, d_workspace, workspace_bytes, stream=None):
-    _here("nanospec_token_logprob", rows.keep and rows.keep[0], d_logprob)
-    _check(lib().nanospec_token_logprob(rows, _ptr(d_logprob), _ptr(d_workspace), workspace_bytes, _stream(stream)), "nanospec_token_logprob")
+    lp, ws = _rows_here("nanospec_token_logprob", _device(), rows, d_logprob, d_workspace)
+    _check(lib().nanospec_token_logprob(rows, lp, ws, workspace_bytes, _stream(stream)), "nanospec_token_logprob")
 
 
-def _grad(rows, d_grad):
+def _grad(where, device, rows, d_grad):
     """(address, type, stride) of a gradient tensor, checked against the rows it belongs to"""
     if d_grad is None:
         return None, F32, 0
+    if d_grad.get_device() != device:
+        _refuse(where, device, d_grad)
     kind, ld = _type_and_stride(d_grad)
     if d_grad.shape[0] < rows.rows or d_grad.shape[1] < rows.V:
         raise ValueError("the gradient has fewer rows or columns than the logits")
@@ -395,11 +416,11 @@ def _grad(rows, d_grad):
 
 def nanospec_policy_loss(rows, d_old, d_ref, d_adv, d_weight, clip_low, clip_high, kl_beta, d_loss, d_row_loss, d_logprob, d_grad, d_workspace,
                          workspace_bytes, grad_scale=1.0, stream=None):
-    _here("nanospec_policy_loss", rows.keep and rows.keep[0], d_loss, d_grad)
-    g, kind, ld = _grad(rows, d_grad)
-    _check(lib().nanospec_policy_loss(rows, _ptr(d_old), _ptr(d_ref), _ptr(d_adv), _ptr(d_weight), clip_low, clip_high, kl_beta, _ptr(d_loss),
-                                      _ptr(d_row_loss), _ptr(d_logprob), g, kind, ld, grad_scale, _ptr(d_workspace), workspace_bytes,
-                                      _stream(stream)), "nanospec_policy_loss")
+    where, device = "nanospec_policy_loss", _device()
+    old, ref, adv, weight, loss, row, lp, ws = _rows_here(where, device, rows, d_old, d_ref, d_adv, d_weight, d_loss, d_row_loss, d_logprob, d_workspace)
+    g, kind, ld = _grad(where, device, rows, d_grad)
+    _check(lib().nanospec_policy_loss(rows, old, ref, adv, weight, clip_low, clip_high, kl_beta, loss, row, lp, g, kind, ld, grad_scale, ws, workspace_bytes,
+                                      _stream(stream)), where)
 
 
 def nanospec_preference_loss(rows, h_off, d_ref, d_weight, beta, smoothing, d_loss, d_margin, d_logprob, d_grad, d_workspace, workspace_bytes,
@@ -408,11 +429,11 @@ def nanospec_preference_loss(rows, h_off, d_ref, d_weight, beta, smoothing, d_lo
     off, op = _off(h_off)
     if off.size % 2 == 0:
         raise ValueError("h_off has a number more than there are answers, which come in pairs")
-    _here("nanospec_preference_loss", rows.keep and rows.keep[0], d_loss, d_grad)
-    g, kind, ld = _grad(rows, d_grad)
-    _check(lib().nanospec_preference_loss(rows, op, off.size // 2, _ptr(d_ref), _ptr(d_weight), beta, smoothing, _ptr(d_loss), _ptr(d_margin),
-                                          _ptr(d_logprob), g, kind, ld, grad_scale, _ptr(d_workspace), workspace_bytes,
-                                          _stream(stream)), "nanospec_preference_loss")
+    where, device = "nanospec_preference_loss", _device()
+    ref, weight, loss, margin, lp, ws = _rows_here(where, device, rows, d_ref, d_weight, d_loss, d_margin, d_logprob, d_workspace)
+    g, kind, ld = _grad(where, device, rows, d_grad)
+    _check(lib().nanospec_preference_loss(rows, op, off.size // 2, ref, weight, beta, smoothing, loss, margin, lp, g, kind, ld, grad_scale, ws, workspace_bytes,
+                                          _stream(stream)), where)
 
 
 def nanospec_last_device_error(st, stream=None) -> int:
