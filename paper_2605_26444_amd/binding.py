@@ -377,6 +377,8 @@ def logit_rows(d_logits, d_tokens, V=None, ids=None, n=None, rows_per_list=1) ->
     kind, ld = _type_and_stride(d_logits)
     if d_tokens.numel() < d_logits.shape[0] or str(d_tokens.dtype) != "torch.int32":
         raise ValueError("a token (int32) for every row of logits is needed")
+    if V is not None and V > d_logits.shape[1]:
+        raise ValueError(f"{V} columns of logits that have {d_logits.shape[1]}")
     device = d_logits.get_device()
     for t in (d_tokens, ids, n):
         if t is not None and not isinstance(t, int) and t.get_device() != device:

@@ -90,3 +90,13 @@ def test_rows_of_logits_of_another_device(call):
         call(there)
     with pytest.raises(B.NanoSpecError):
         call(rows())
+
+
+@pytest.mark.parametrize("shape,stride", [((4, 32), None), ((4, 32), (64, 1)), ((1, 32), (64, 1))])
+def test_no_more_columns_than_the_logits_have(shape, stride):
+    """a wider row stride, or a single row, is no room for more columns: the last row's would lie behind the tensor"""
+    z, t = Stub(shape=shape, stride=stride), Stub(shape=(4,), dtype=torch.int32)
+    assert B.logit_rows(z, t).V == 32 and B.logit_rows(z, t, V=31).V == 31
+    for V in (33, 64):
+        with pytest.raises(ValueError, match="columns"):
+            B.logit_rows(z, t, V=V)
