@@ -360,7 +360,8 @@ typedef struct nanospec_logit_rows {
  *     row_loss[r] = -min(ratio A, clamp(ratio, 1 - clip_low, 1 + clip_high) A) + kl_beta (exp(gap) - gap - 1),
  *     loss = sum of w_r row_loss[r] over the rows that count (a mean over tokens or answers is a matter of the weights).
  *     d_ref may be NULL if kl_beta is 0.  A row whose token has no probability, or one that is 0 in 64 bits (a log-probability
- *     below -745, of which ratio and KL term take the exponential), has row_loss 0 and no gradient.
+ *     below -745, of which ratio and KL term take the exponential), has row_loss 0 and no gradient.  d_old may be -inf: the ratio
+ *     is infinite then, and its product with an advantage of 0 is 0.
  *   nanospec_preference_loss: the preference loss on `pairs` pairs of answers.  Answer q covers rows h_off[q] .. h_off[q+1), pair p
  *     is answer 2p, the chosen one, and 2p + 1, the rejected one; rows outside h_off[0] .. h_off[2 pairs) do not count;
  *     S_q = sum of w_r (log p_r - d_ref[r]) (d_ref NULL: 0; every finite log p_r counts, also that of a token masked with a finite

@@ -323,7 +323,9 @@ struct PolicyRow {
 __device__ __forceinline__ PolicyRow policy_row(const PolicyArgs& a, int row, double lp) {
   const double adv = a.adv[row], ratio = exp(lp - (double)a.old[row]);
   const double lo = 1.0 - (double)a.clip_low, hi = 1.0 + (double)a.clip_high;
-  const double held = (ratio < lo ? lo : ratio > hi ? hi : ratio) * adv, free = ratio * adv;
+  // old may be -inf, or so low that the ratio does not fit: an advantage of 0 makes nothing of it
+  auto times = [&](double x) { return adv == 0.0 && x == INFINITY ? 0.0 : x * adv; };
+  const double held = times(ratio < lo ? lo : ratio > hi ? hi : ratio), free = times(ratio);
   PolicyRow r{-(free <= held ? free : held), free <= held ? -free : 0.0};
   if (free != free) r.loss = r.c = free;                   // NaN stays NaN
   if (a.ref) {

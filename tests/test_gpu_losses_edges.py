@@ -191,3 +191,26 @@ def test_preference_without_a_gradient(rows, V, off, kind):
         # margins and losses are added by workgroups of another size there
         T.near(beside["margin"][:-1], margin, mb, "margin")
         T.near(beside["loss"][:1], [loss], [lb], "loss")
+
+
+@pytest.mark.parametrize("rows,V", [(6, 50), (6, 9001), (130, 9001), (300, 50)])
+def test_a_ratio_without_end(rows, V):
+    """a policy before that gave the token no probability (-inf) or hardly one: with an advantage of 0 the row adds its KL term, with a positive one the clipped term"""
+    g, z, t = T.logits(rows, rows, V, "f32")
+    old, ref, adv = T.policy_inputs(g, z, t, rows)
+    old[:4] = [-np.inf, -900.0, -np.inf, -900.0]
+    adv[:4] = [0.0, 0.0, 0.5, 0.5]
+    grad = torch.full((rows, V), 9.0, device="cuda")
+    got = T.run_policy(z.cuda(), t, old, ref, adv, None, 0.05, grad)
+    want = L.rows64(z.double().numpy(), t)
+    near_old = old.copy()
+    near_old[:4] = np.float32(T.lp_of(want)[:4] - 5)          # a ratio beyond the clip for which the formula needs no limit
+    loss, lb, row, rb, dlp, slack = L.policy(want, near_old, ref, adv, None, 0.2, 0.28, 0.05)
+    T.near(got["row"][:rows], row, rb, "rows")
+    T.near(got["loss"][:1], [loss], [lb], "loss")
+    gg = grad.cpu().numpy()
+    for r, (x, b) in enumerate(L.gradient(want, [V] * rows, dlp, slack)):
+        T.near(gg[r], x, b, r)
+    z[1, 0] = np.nan                                        # and a NaN is none of these
+    got = T.run_policy(z.cuda(), t, old, ref, adv, None, 0.05, grad)
+    assert np.isnan(got["row"][1]) and np.isfinite(np.delete(got["row"][:rows], 1)).all() and np.isnan(got["loss"][0])
