@@ -374,8 +374,8 @@ typedef struct nanospec_logit_rows {
  *   d_grad : NULL: none.  Else [rows][ld_grad] of grad_type: grad_scale * dloss/dz for every row and its live columns, zeros in rows
  *     that do not count.  It may be the logits' own memory if type and stride are the same, and must not share their range of addresses else.
  *     No other output may share memory with an input.
- *   d_workspace : device scratch of at least nanospec_loss_workspace(rows, V) bytes (-1: sizes out of range), 256-byte aligned.  Calls
- *     that may overlap must not share one.
+ *   d_workspace : device scratch of at least nanospec_loss_workspace(rows, V) bytes (-1: sizes out of range), 256-byte aligned; what is
+ *     enough for some rows and columns is enough for fewer.  Calls that may overlap must not share one.
  * Limits: rows <= 2^22, rows * ld below 2^60, V <= 2^30; logits and gradients aligned to their type.  Errors: EINVAL (null, sizes < 1, ld < V, an unknown type, d_ids without d_n or
  * the other way round, clip_low or clip_high negative, kl_beta != 0 without d_ref, smoothing outside [0, 1], a NaN among these, bad
  * offsets), ECAPACITY (workspace too small, 2 pairs > NANOSPEC_MAX_BATCH), EHIP.  Asynchronous. */

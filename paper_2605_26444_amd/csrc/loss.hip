@@ -725,6 +725,13 @@ static RowCut stats_cut(int32_t rows, int32_t V) { return whole_threads(rows, V)
 
 static int64_t up256(int64_t x) { return (x + 255) / 256 * 256; }
 
+// No less than rows * row_cut(rows, V).pieces, and no more for fewer rows or columns, so that a workspace of a program's largest batch is enough for the others (pieces fall as rows
+// rise: 2047 rows have twice as many as 2048).
+static int64_t most_pieces(int32_t rows, int32_t V) {
+  const int64_t by_columns = (int64_t)rows * (((int64_t)V + 4095) / 4096), by_rows = (int64_t)rows + 2047;
+  return by_columns < by_rows ? by_columns : by_rows;
+}
+
 struct LossSpace {
   Stat* part;
   Place* at;
@@ -735,7 +742,7 @@ struct LossSpace {
 static LossSpace loss_space(char* p, int32_t rows, int32_t V) {
   LossSpace s;
   s.part = reinterpret_cast<Stat*>(p);
-  p += up256((int64_t)rows * row_cut(rows, V).pieces * sizeof(Stat));
+  p += up256(most_pieces(rows, V) * sizeof(Stat));
   s.coef = reinterpret_cast<RowCoef*>(p);
   p += up256((int64_t)rows * sizeof(RowCoef));
   s.term = reinterpret_cast<double*>(p);
@@ -745,7 +752,7 @@ static LossSpace loss_space(char* p, int32_t rows, int32_t V) {
 }
 
 int64_t loss_workspace_bytes(int32_t rows, int32_t V) {
-  return up256((int64_t)rows * row_cut(rows, V).pieces * sizeof(Stat)) + up256((int64_t)rows * sizeof(RowCoef)) + up256((int64_t)rows * sizeof(double)) +
+  return up256(most_pieces(rows, V) * sizeof(Stat)) + up256((int64_t)rows * sizeof(RowCoef)) + up256((int64_t)rows * sizeof(double)) +
          up256((int64_t)rows * sizeof(Place));
 }
 
