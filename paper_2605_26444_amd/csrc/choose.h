@@ -173,9 +173,11 @@ inline FewPlan few_plan(int32_t M, int32_t d, int32_t batch, int32_t cap_rows, b
 
 // ---- losses (loss.hip) --------------------------------------------------------------------------------------------
 
-// Whether a row's loss and gradient are one workgroup's, which reads the row once, or the chip's in pieces, twice (us, fp32 logits to bf16, apart / one workgroup): 128256
-// columns, 128 rows 34.5 / 31.3, 256 64 / 52.5, 300 78 / 79 (the last 44 rows have the chip to themselves), 2048 518 / 341; 32000, 128 15.4 / 14.6, 2048 135 / 91; 8000, 128 11.7 /
-// 10.2, 2048 37 / 35; 1000, 128 12.2 / 12.6, 2048 17.2 / 20.0; 152064, of which 21000 columns are read twice, 2048 612 / 430.
+// Whether a row's loss and gradient are one workgroup's, which reads the row once, or the chip's in pieces, twice (us in a graph, fp32 logits to bf16, apart / one workgroup): 128256
+// columns, 129 rows 34.3 / 32.2, 200 55 / 43, 300 86 / 76 (the last 44 rows have the chip to themselves), 2048 481 / 330; 32000, 129 16.4 / 13.8, 2048 129 / 89; 8000, 129 10.2 /
+// 8.6, 600 17.5 / 17.0, 2048 38.4 / 39.2; 4096, 129 8.8 / 7.4, 600 13.9 / 12.7, 2048 24.2 / 26.8; 1000, 128 6.6 / 6.6, 2048 17.6 / 19.8; 152064, of which 21000 columns are read
+// twice, 2048 574 / 431.  At 128 rows, which are two launches apart, the same within 8 %: 128256 31.3 / 32.0, 32000 14.0 / 13.7, 8000 8.9 / 8.9.  bf16 to bf16: 128256, 129 26.5 / 28.6,
+// 2048 318 / 252; 32000, 2048 93 / 71; 8000, 129 9.8 / 7.8, 2048 29.6 / 30.7.
 inline bool policy_fuses(int32_t rows, int32_t V) { return rows >= 128 && V >= 4096; }
 
 // The 8-bit head's block shapes beyond: as many bytes a step hold twice the columns, so that a block's walk is half as many steps and larger blocks pay earlier than above.  By the work, rows (what the

@@ -24,7 +24,8 @@ typedef __bf16 bf16x8_any __attribute__((ext_vector_type(8), aligned(2)));
 
 constexpr int kRowThreads = 256;         // of a workgroup that takes a piece of a row
 // log2 e lies between two fp32 numbers, 0.16 of their distance above the lower one.  With one of them for all exponents, every term of a row's sum is off by 1.3e-8 (or 7e-8) of
-// its exponent to the same side, which does not average out (1e-7 of the sum; seen in the margin of two answers, where most of the log-probabilities cancel).
+// its exponent to the same side, which does not average out (1e-7 of the sum; seen in the margin of two answers, where most of the log-probabilities cancel).  The sums
+// therefore use both.  A gradient's entry is one probability, in which nothing cancels: it takes the lower one, whose 1.3e-8 is a fifth of the exponent's own rounding.
 constexpr float kLog2e = 0x1.715476p+0f, kLog2eUp = 0x1.715478p+0f, kLog2eRest = 0x1.4ae0c0p-26f, kLn2 = 0.6931471805599453f;   // kLog2e + kLog2eRest: log2 e
 
 // x <= 0, between two maxima, for the sums: the exponent rounded once
@@ -381,8 +382,8 @@ __global__ __launch_bounds__(1024) void policy_sum_kernel(int rows, const double
 
 // A row's policy loss and its gradient by one workgroup, which keeps the row on the compute unit between the two: RC pieces of 16 bytes a thread in
 // registers, LC in LDS, so that up to (RC + LC) 8 KB of a row are read from memory once; what is beyond is read a second time, from
-// the caches.  Two launches over all rows instead read them twice from memory: 2048 rows of 128256, fp32 to bf16, 518 us apart, 322 so (4.9 TB/s read and written, as a
-// copy; 512 KB of a row fit the compute unit's 672 of registers and LDS); to fp32 621 / 421.  Eight wavefronts, not sixteen: 256 registers a lane instead of 128.
+// the caches.  Two launches over all rows instead read them twice from memory: 2048 rows of 128256, fp32 to bf16, 481 us apart, 330 so (4.8 TB/s read and written, near a
+// copy; 512 KB of a row fit the compute unit's 672 of registers and LDS), bf16 to bf16 318 / 252, fp32 to fp32 420 so.  Eight wavefronts, not sixteen: 256 registers a lane instead of 128.
 // A chunk is what the workgroup's threads hold in a piece each; a row's full chunks go to LDS first, then to registers, the others and the row's end are streamed.
 template <typename T, typename G, int RC, int LC>
 __global__ __launch_bounds__(512, 2) void policy_fused_kernel(const LogitRows r, const PolicyArgs a, double* __restrict__ term, G* grad, int64_t ld_grad) {

@@ -606,8 +606,10 @@ static hipError_t run_gemm(const uint16_t* W, const uint16_t* H, const int32_t* 
 }
 
 // The 8-bit head: rows in pairs of columns (d2 = d / 2), the hidden rows quantized, the same block shapes.  Bound as in bf16, by the bytes a compute unit has in flight or HBM, with half the bytes: 3000
-// rows of 3584, M = 64 8.2 us (bf16 11.1), 128256 x 4096, M = 64 134 (205).  head_gemm_i8_kernel: 1024 hidden rows on 128256 x 4096 470 us = 2.3 POP/s, matrix cores busy 0.57 of the cycles, as
-// in bf16 (896 us); the scales, fetched straight into LDS with the operands instead of before them, changed nothing.
+// rows of 3584, M = 64 8.2 us (bf16 11.1), 128256 x 4096, M = 64 134 (205; the bytes 92: a block of 64 rows fetches as many bytes of hidden rows as of W, from L2, so that half of what it has in
+// flight is not HBM's; on one chip M = 16 108, 17 118, 32 122, 64 137).  head_gemm_i8_kernel: 1024 hidden rows on 128256 x 4096 478 to 493 us with the hidden rows' 6 = 2.2 POP/s, matrix cores busy
+// 0.64 of the compute units' busy cycles, 0.56 of the launch's; head_gemm_kernel 0.71 and 0.65.  A step is 2048 cycles of matrix instructions a SIMD and 2048 of LDS (192 KB out, 64 KB in, at
+// 128 bytes a cycle) in either, so neither is idle while the other works only if they overlap wholly.  The scales, fetched straight into LDS with the operands instead of before them, changed nothing.
 template <int WR, int WH, int FR, int FH, int BK, int D, bool TAIL>
 __global__ __launch_bounds__(64 * WR * WH) void head_wide_i8_kernel(const ProductI8 product, const uint16_t* __restrict__ W, const uint16_t* __restrict__ H,
                                                            const int32_t* __restrict__ ids, const int32_t* __restrict__ n_dev, int n_fixed, int V, int batch,
