@@ -214,3 +214,80 @@ def test_a_ratio_without_end(rows, V):
     z[1, 0] = np.nan                                        # and a NaN is none of these
     got = T.run_policy(z.cuda(), t, old, ref, adv, None, 0.05, grad)
     assert np.isnan(got["row"][1]) and np.isfinite(np.delete(got["row"][:rows], 1)).all() and np.isnan(got["loss"][0])
+
+
+def strided(z, kind, lead, wide):
+    """z in the columns lead .. of rows of `wide` columns, 7 around it"""
+    buf = torch.full((z.shape[0], wide), 7.0, dtype=T.KIND[kind], device="cuda")
+    buf[:, lead:lead + z.shape[1]] = z.cuda()
+    return buf, buf[:, lead:lead + z.shape[1]]
+
+
+@pytest.mark.parametrize("kind,grad_kind,inplace", [("f32", "f32", True), ("f32", "bf16", False), ("bf16", "bf16", True), ("bf16", "f32", False)])
+@pytest.mark.parametrize("rows,V", [(130, 4099), (128, 17003), (128, 66001), (129, 140003)])
+def test_strided_rows_that_one_workgroup_holds(rows, V, kind, grad_kind, inplace):
+    """rows that start at odd elements, with columns of others between them: policy loss, preference loss and log-probabilities"""
+    g, z, t = T.logits(rows + V, rows, V, kind)
+    old, ref, adv = T.policy_inputs(g, z, t, rows)
+    w = T.weights(g, rows)
+    for loss in ("policy", "preference"):
+        buf, view = strided(z, kind, 3, V + 11)
+        gbuf, gview = (buf, view) if inplace else strided(torch.zeros_like(z), grad_kind, 5, V + 8)
+        if loss == "policy":
+            want = L.rows64(z.double().numpy(), t, weight=w)
+            got = T.run_policy(view, t, old, ref, adv, w, 0.05, gview)
+            total, bound, _, _, dlp, slack = L.policy(want, old, ref, adv, w, 0.2, 0.28, 0.05)
+        else:
+            off = [2, 50, 60, 61, rows - 3]
+            want = L.rows64(z.double().numpy(), t, weight=w, inside=(np.arange(rows) >= 2) & (np.arange(rows) < rows - 3))
+            got = T.run_preference(view, t, off, ref, w, 0.2, 0.1, gview)
+            total, bound, _, _, dlp, slack = L.preference(want, off, ref, w, 0.2, 0.1)
+        T.near(got["lp"][:rows], T.lp_of(want), T.lp_bound(want), "logprob")
+        T.near(got["loss"][:1], [total], [bound], "loss")
+        gg, lead = gbuf.float().cpu().numpy(), 3 if inplace else 5
+        for r, (x, b) in enumerate(L.gradient(want, [V] * rows, dlp, slack, 1.0, T.NAME[T.KIND[grad_kind]])):
+            T.near(gg[r, lead:lead + V], x, b, r)
+        assert (gg[:, :lead] == 7).all() and (gg[:, lead + V:] == 7).all()
+        if not inplace:
+            assert torch.equal(view, z.cuda()) and (buf[:, :3] == 7).all() and (buf[:, 3 + V:] == 7).all()
+
+
+@pytest.mark.parametrize("counts,M,off", [([5, 0, 64, 700], 3, [0, 2, 4, 7, 12]), ([2300] * 5, 8, [1, 9, 20, 33, 38]), ([9000, 0, 1, 4100, 8192] * 5, 7, [0, 80, 174]), ([300, 299, 7] * 100, 2, [0, 290, 600]),
+                                          ([33000, 20000], 70, [0, 30, 71, 90, 139]), ([1], 1, [0, 1, 1])])
+def test_preference_over_active_sets(counts, M, off):
+    """pairs of answers on the active sets' logits, with tokens that the sets do not hold; columns behind the live ones are neither read nor written"""
+    V, batch = 40009, len(counts)
+    g = np.random.RandomState(M + batch)
+    cap = (max(counts) + 64) // 64 * 64
+    ids = [np.sort(g.permutation(V)[:n]).astype(np.int32) for n in counts]
+    lists = np.full((batch, cap), -5, np.int32)
+    for b, x in enumerate(ids):
+        lists[b, :len(x)] = x
+    rows = batch * M
+    z = torch.from_numpy((g.randn(rows, cap) * 2).astype(np.float32))
+    t = np.array([ids[r // M][g.randint(counts[r // M])] if counts[r // M] and r % 5 != 3 else g.randint(V) for r in range(rows)], np.int32)
+    live = [z[r, :counts[r // M]].double().numpy() for r in range(rows)]
+    zd = z.cuda()
+    for r in range(rows):
+        zd[r, counts[r // M]:] = float("nan")
+    src = B.logit_rows(zd, T.dev(t, torch.int32), ids=T.dev(lists, torch.int32), n=T.dev(counts, torch.int32), rows_per_list=M)
+    inside = (np.arange(rows) >= off[0]) & (np.arange(rows) < off[-1])
+    want = L.rows64(live, t, ids=[ids[r // M] for r in range(rows)], inside=inside)
+    lp = T.lp_of(want)
+    ref = (np.where(np.isfinite(lp), lp, -1.0) + g.randn(rows) * 0.4).astype(np.float32)
+    loss, lb, margin, mb, dlp, slack = L.preference(want, off, ref, None, 0.2, 0.1)
+    grad = torch.full((rows, cap), 9.0, device="cuda")
+    for gr in (grad, None):
+        got = T.run_preference(zd, t, off, ref, None, 0.2, 0.1, gr, rows=src)
+        T.near(got["lp"][:rows], lp, T.lp_bound(want), "logprob")
+        T.near(got["margin"][:-1], margin, mb, "margin")
+        T.near(got["loss"][:1], [loss], [lb], "loss")
+    gg = grad.cpu().numpy()
+    for r, (x, b) in enumerate(L.gradient(want, [len(a) for a in live], dlp, slack)):
+        T.near(gg[r, :len(live[r])], x, b, r)
+        assert (gg[r, len(live[r]):] == 9.0).all()
+    every = L.rows64(live, t, ids=[ids[r // M] for r in range(rows)])
+    out = torch.empty(rows, device="cuda")
+    ws, n = T.space(rows, cap)
+    B.nanospec_token_logprob(src, out, ws, n)
+    T.near(out.cpu(), T.lp_of(every), T.lp_bound(every), "logprob of all rows")
